@@ -346,6 +346,150 @@ int ersd_optimal_tree(const double* accept, int max_children, int k, int32_t* pa
 int ersd_acceptance_profile(const int32_t* paths, const int32_t* parent, int B, int N, int max_children,
                             double* accept, int64_t* trials);
 
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Around a verification: the target model's attention over the drafted rows, the paged cache that
+ * it reads, and what is done to logits before they are raced.
+ * ------------------------------------------------------------------------------------------------
+ * A cache holds keys and values in pages of page_size positions; position p of sequence b is row
+ * p % page_size of page block_table[b, p / page_size].  context_lens[b] positions are there before
+ * the call's rows; row (node) n of a call has slot context_lens[b] + n.  For a chain and for rows of
+ * a prompt the slot is the position; in a draft tree (`parent` as for ersd_verify_tree) the position
+ * of node n, by which windows and first tokens are counted, is context_lens[b] + depth(n).
+ * Slots beyond max_pages * page_size do not exist, and a page outside [0, num_pages) is never
+ * touched: rows for them are not written, and as keys the slots of such a page count as zeros.
+ * Lengths below 0 count as 0.  Strides are in elements; the innermost dimension is contiguous.
+ * These calls need no workspace, allocate nothing and can be captured.
+ */
+typedef struct ersd_cache {
+  uint32_t struct_size;   /* sizeof(ersd_cache) */
+  uint32_t dtype;         /* ersd_dtype of keys, values and the rows that go with them */
+  void* k;                /* device: element d of head h, row t, page p, layer l at
+                             l*k_stride_layer + p*k_stride_page + t*k_stride_token + h*k_stride_head + d */
+  void* v;
+  int32_t num_pages, page_size, heads, head_dim;
+  int32_t layers;         /* ersd_cache_commit moves this many; the other calls take the first */
+  int32_t max_pages;      /* entries of a sequence in block_table */
+  const int32_t* block_table; /* device [B, max_pages], table_stride entries apart */
+  int64_t table_stride;
+  int64_t k_stride_layer, k_stride_page, k_stride_token, k_stride_head;
+  int64_t v_stride_layer, v_stride_page, v_stride_token, v_stride_head;
+} ersd_cache;
+
+#define ERSD_MAX_HEAD_DIM 256 /* ersd_chunk_attention: largest head_dim */
+
+/* Options of the calls over a cache; NULL = defaults.  Set struct_size = sizeof(ersd_chunk_opts). */
+typedef struct ersd_chunk_opts {
+  uint32_t struct_size;
+  float scale;               /* attention: factor of q.k before the softmax; 0 = 1 / sqrt(head_dim) */
+  const int32_t* parent;     /* HOST [R], nullable: draft tree of the rows; NULL = every row follows the one before */
+  const int32_t* row_counts; /* device [B], nullable: rows of sequence b (at most R count; NULL = R).  Rows
+                                behind them are neither read nor written */
+  int32_t window;            /* attention: 0, or a key is visible only if its position is > the row's - window ... */
+  int32_t sinks;             /* ... or < sinks */
+  int32_t max_context;       /* attention: 0, or an upper bound of context_lens: only speeds the call up */
+  int32_t split;             /* attention: thread blocks that share a tile of rows, 1, 2, 4, 8, 16; 0 = chosen by the library */
+  uint32_t kernel_path;      /* attention: 0 = chosen by the library, 1 = the kernel of 32-bit arithmetic, 2 = the kernel of
+                                tensor-core products (ERSD_EUNSUPPORTED where it does not apply: see below) */
+  uint32_t reserved;
+  int64_t a_stride_b, a_stride_r, a_stride_h; /* strides of q / k_new in sequences, rows, heads; all 0 = contiguous */
+  int64_t b_stride_b, b_stride_r, b_stride_h; /* the same of out / v_new */
+} ersd_chunk_opts;
+
+/*
+ * Attention of a chunk of new rows over a paged cache: the evaluation of a drafted chain or tree by
+ * the target model in one pass (the paper's "one length-(n+k) pass", its footnote on SpecInfer), of
+ * a single token (R = 1), or of a piece of a prompt.  The rows' own keys and values are in the
+ * cache already (ersd_cache_append).  For row n of sequence b and query head h, over the keys p that
+ * it sees, with the kv head h / (Hq / heads):
+ *     out = sum_p softmax_p(scale * q . k_p) v_p.
+ * Row n sees the slots below context_lens[b], itself and: every row before it (parent NULL) or its
+ * ancestors (a tree); of these, with a window, those whose position is > its own - window or < sinks.
+ * A row that sees nothing gets zeros.  Slots that no row of a call sees do not enter, whatever they
+ * hold, and pages of such slots alone are not read.
+ *   q device [B, R, Hq, head_dim]   out device [B, R, Hq, head_dim]   of cache->dtype, not overlapping
+ *   context_lens device [B] int32
+ * Scores, softmax and sums are 32-bit.  bfloat16 caches with head_dim 64 or 128, page_size a multiple
+ * of 8, k and v on 16-byte boundaries in every stride run on tensor cores, with the softmax weights
+ * rounded to bfloat16 for the second product; the rest on 32-bit arithmetic.
+ * Errors: ERSD_EINVAL (null pointers, sizes < 1, Hq not a multiple of heads, window or sinks < 0, bad
+ * parent, scale not finite); ERSD_EALIGN (a pointer off its element size); ERSD_EUNSUPPORTED for
+ * head_dim > ERSD_MAX_HEAD_DIM, a tree of more than ERSD_MAX_ROWS rows, B or heads > 65535, R * Hq or
+ * max_pages * page_size beyond 2^30.
+ */
+int ersd_chunk_attention(const ersd_cache* cache, const void* q, void* out, const int32_t* context_lens, int B, int R, int Hq,
+                         const ersd_chunk_opts* opts, void* cuda_stream);
+
+/*
+ * Writes the keys and values of new rows into their slots: k_new, v_new device [B, R, heads, head_dim]
+ * (strides a_*, b_* of the options), row r of sequence b into slot context_lens[b] + r.  No two
+ * sequences may share the pages that are written.  Errors as above; `parent`, window, sinks, scale,
+ * max_context, split and kernel_path are not looked at.
+ */
+int ersd_cache_append(const ersd_cache* cache, const void* k_new, const void* v_new, const int32_t* context_lens, int B, int R,
+                      const ersd_chunk_opts* opts, void* cuda_stream);
+
+/*
+ * After ersd_verify_tree (or ersd_gsd_verify_tree): makes the accepted path of a draft tree the
+ * sequence's own, in all layers, with one launch.  For every j <= accept_len[b] the keys and values
+ * of node path[b, j] move from slot context_lens[b] + path[b, j] to slot context_lens[b] + j.
+ *   path device [B, D+1] int32: opts->out_path of the verification (ascending, from node 0)
+ *   accept_len device [B] int32; accept_len < 0 moves nothing
+ *   out_context_lens device [B] int32, nullable, not context_lens itself: context_lens[b] + accept_len[b] + 1
+ * Errors as above.
+ */
+int ersd_cache_commit(const ersd_cache* cache, const int32_t* context_lens, const int32_t* path, const int32_t* accept_len, int B,
+                      int D, int32_t* out_context_lens, void* cuda_stream);
+
+/* What ersd_process_logits does to a row.  Set struct_size = sizeof(ersd_logit_opts); what is NULL is left out. */
+typedef struct ersd_logit_opts {
+  uint32_t struct_size;
+  int32_t history_width;        /* entries of a sequence in `history` */
+  int64_t ld_in, ld_out;        /* row strides in elements; 0 = V */
+  const int32_t* history;       /* device [B, history_width]: tokens of the sequence so far, prompt first */
+  const int32_t* history_lens;  /* device [B]: how many of them count; NULL = history_width */
+  const int32_t* prompt_lens;   /* device [B]: how many of these are the prompt; NULL = 0 */
+  const int32_t* draft_tokens;  /* device: chain [B, R-1], entry j = token drafted at position j (row j + 1 follows
+                                   it); tree [B, R], entry n = token drafted at node n (entry 0 unused) */
+  const int32_t* parent;        /* HOST [R]: draft tree of the rows; NULL = chain */
+  const float* repetition;      /* device [B]; > 0 */
+  const float* presence;        /* device [B] */
+  const float* frequency;       /* device [B] */
+  const int32_t* bias_tokens;   /* device [B, bias_count] (bias_stride apart, 0 = the same for all sequences) */
+  const float* bias_values;     /* the same shape */
+  int64_t bias_stride;
+  const uint32_t* mask;         /* device: bit i & 31 of word i >> 5 of row (b, r) set = token i allowed; rows
+                                   mask_stride_b and mask_stride_r words apart (0 = shared) */
+  int64_t mask_stride_b, mask_stride_r;
+  int32_t bias_count;
+  uint32_t reserved;
+} ersd_logit_opts;
+
+#define ERSD_MAX_BIASES 65535 /* ersd_process_logits: largest bias_count */
+
+/*
+ * Penalties, biases and masks on logits, for the rows of a race or verify call, in one launch.  For
+ * token i of row n, with c = occurrences of i among the history behind the prompt and on the path
+ * of drafted tokens that leads to row n, and i "seen" if c > 0 or i is in the prompt:
+ *     l = l > 0 ? l / repetition : l * repetition     if seen
+ *     l = l - frequency * c - presence * [c > 0]
+ *     l = l + bias
+ *     l = -inf                                        if the mask's bit is 0
+ * in 32-bit arithmetic, rounded once to the logits' type.  Row n of a chain follows draft tokens
+ * 0..n-1; row n of a tree those of the path from the root to n.  Tokens outside [0, V) in the
+ * history, the drafts or the biases count for nothing; of a token listed twice among a sequence's
+ * biases the later entry counts.  A masked token is -inf whatever its logit; a row whose mask allows nothing is
+ * all -inf, for which a race yields token -1.
+ *   logits device [B, R, V]   out device [B, R, V] of the same type: other memory, or `logits`
+ *   itself with the same row stride (tokens that nothing changes are then neither read nor written)
+ * Entries V..ld-1 of a row are left alone.
+ * Errors: ERSD_EINVAL (null pointers, sizes < 1, strides below V, draft_tokens or parent that do not
+ * go with R, values without tokens, ...); ERSD_EALIGN; ERSD_EUNSUPPORTED for B > 65535, draft tokens
+ * with R > ERSD_MAX_ROWS, V > 0x7FFF0000, bias_count > ERSD_MAX_BIASES.
+ */
+int ersd_process_logits(const void* logits, void* out, ersd_dtype dt, int B, int R, int V, const ersd_logit_opts* opts,
+                        void* cuda_stream);
+
 /* Depth (longest root-to-leaf edge count) of a HOST parent array, or -1 if it is malformed. */
 int ersd_tree_depth(const int32_t* parent, int N);
 

@@ -25,7 +25,7 @@ ERSD_NOALLOC_MAX_ROWS = 1024
 ERSD_ENOALLOC_LIMIT = -6
 
 EXPORTS = ("ersd_race_sample", "ersd_verify", "ersd_verify_tokens", "ersd_verify_noalloc", "ersd_verify_tree", "ersd_gsd_verify", "ersd_gsd_verify_tree", "ersd_tree_depth", "ersd_optimal_tree",
-           "ersd_acceptance_profile", "ersd_row_keys", "ersd_workspace_bytes", "ersd_workspace_init", "ersd_status_string",
+           "ersd_acceptance_profile", "ersd_chunk_attention", "ersd_cache_append", "ersd_cache_commit", "ersd_process_logits", "ersd_row_keys", "ersd_workspace_bytes", "ersd_workspace_init", "ersd_status_string",
            "ersd_last_cuda_error", "ersd_last_launch", "ersd_version")
 
 
@@ -115,7 +115,8 @@ def native():
                                "paper_2504_15475_b200.build`" % (built_for, torch.__version__))
         _ersd_call.use(*[C.cast(f, C.c_void_p).value for f in (
             L.ersd_race_sample, L.ersd_verify, L.ersd_verify_noalloc, L.ersd_verify_tokens, L.ersd_verify_tree,
-            L.ersd_gsd_verify, L.ersd_gsd_verify_tree)], ErsdOpts)
+            L.ersd_gsd_verify, L.ersd_gsd_verify_tree, L.ersd_chunk_attention, L.ersd_cache_append, L.ersd_cache_commit,
+            L.ersd_process_logits)], ErsdOpts)
         _native = _ersd_call
     return _native
 
@@ -310,6 +311,61 @@ def ersd_verify_tree(target_logits: torch.Tensor, draft_logits: Optional[torch.T
                                                stream, V)
     if status:
         raise ErsdError(status, "ersd_verify_tree")
+
+
+def ersd_chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                         context_lens: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
+                         parent: Optional[Sequence[int]] = None, row_counts: Optional[torch.Tensor] = None,
+                         window: int = 0, sinks: int = 0, max_context: int = 0, split: int = 0, kernel_path: int = 0,
+                         stream=None) -> None:
+    """Attention of new rows over a paged cache that already holds their keys and values.
+    q, out [B, R, Hq, D]; k_cache, v_cache [pages, page_size, heads, D] (all of one type, bf16 or f32, any strides
+    with D contiguous); block_table int32 [B, entries]; context_lens int32 [B]: positions before the rows.
+    parent: host list [R], the rows are a draft tree; None: each follows the one before.  row_counts int32 [B]:
+    rows that count.  window, sinks: see only the last `window` positions and the first `sinks`.  max_context: an
+    upper bound of context_lens, for speed alone."""
+    status = (_native or native()).chunk_attention(q, k_cache, v_cache, block_table, context_lens, out, scale, parent,
+                                                   row_counts, window, sinks, max_context, split, kernel_path, stream)
+    if status:
+        raise ErsdError(status, "ersd_chunk_attention")
+
+
+def ersd_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      block_table: torch.Tensor, context_lens: torch.Tensor, row_counts: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """Keys and values [B, R, heads, D] of new rows into slots context_lens[b] + r of the cache."""
+    status = (_native or native()).cache_append(k_new, v_new, k_cache, v_cache, block_table, context_lens, row_counts, stream)
+    if status:
+        raise ErsdError(status, "ersd_cache_append")
+
+
+def ersd_cache_commit(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor,
+                      path: torch.Tensor, accept_len: torch.Tensor, out_context_lens: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """After a tree verification: the accepted nodes' keys and values (path int32 [B, D+1]: its opts.out_path) move
+    to the slots behind the context, in all layers of caches [layers, pages, page_size, heads, D] (or one, without
+    the first dimension); out_context_lens int32 [B] = context_lens + accept_len + 1."""
+    status = (_native or native()).cache_commit(k_cache, v_cache, block_table, context_lens, path, accept_len, out_context_lens,
+                                                stream)
+    if status:
+        raise ErsdError(status, "ersd_cache_commit")
+
+
+def ersd_process_logits(logits: torch.Tensor, out: torch.Tensor, history: Optional[torch.Tensor] = None,
+                        history_lens: Optional[torch.Tensor] = None, prompt_lens: Optional[torch.Tensor] = None,
+                        draft_tokens: Optional[torch.Tensor] = None, parent: Optional[Sequence[int]] = None,
+                        repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                        frequency: Optional[torch.Tensor] = None, bias_tokens: Optional[torch.Tensor] = None,
+                        bias_values: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                        V: Optional[int] = None, stream=None) -> None:
+    """Penalties, biases and masks on logits [B, R, V] (f32/bf16) before a race or verification; out: other memory of
+    that shape, or `logits` itself.  history int32 [B, width] with history_lens / prompt_lens int32 [B]; draft_tokens
+    int32 [B, R-1] of a chain or, with `parent`, [B, R] of a tree; repetition, presence, frequency float32 [B];
+    bias_tokens int32 and bias_values float32 [B or 1, n]; mask int32 [B or 1, R or 1, ceil(V / 32)], bit set = allowed."""
+    status = (_native or native()).process_logits(logits, out, history, history_lens, prompt_lens, draft_tokens, parent, repetition,
+                                                  presence, frequency, bias_tokens, bias_values, mask, V, stream)
+    if status:
+        raise ErsdError(status, "ersd_process_logits")
 
 
 def ersd_row_keys(row: torch.Tensor, T: float, seed: int, seq_id: int, position: int, mode: int,

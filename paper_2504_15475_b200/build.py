@@ -10,9 +10,11 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SRC = [os.path.join(CSRC, name) for name in ("ersd.cu", "ersd_cluster_bf16.cu", "ersd_cluster_f32.cu", "ersd_tree.cpp")]
+SRC = [os.path.join(CSRC, name) for name in ("ersd.cu", "ersd_cluster_bf16.cu", "ersd_cluster_f32.cu", "ersd_attention.cu", "ersd_cache.cu",
+                                                   "ersd_logits.cu", "ersd_tree.cpp")]
 DEPS = SRC + [os.path.join(CSRC, name) for name in ("ersd_device.cuh", "ersd_math.cuh", "ersd_kernel.inc", "ersd_cluster.inc",
-                                                    "ersd_cluster_top.inc", "ersd_cluster_select.inc", "ersd_gsd.inc")]
+                                                    "ersd_cluster_top.inc", "ersd_cluster_select.inc", "ersd_gsd.inc", "ersd_host.h",
+                                                    "ersd_attention.cuh")]
 DEPS.append(os.path.join(ROOT, "include", "ersd.h"))
 LIB = os.path.join(HERE, "libersd.so")
 CALL_SRC = os.path.join(HERE, "csrc", "ersd_call.cpp")

@@ -12,6 +12,7 @@
 // (sequence scan or tree walk) in the same launch.
 #include <cuda_runtime.h>
 #include <math.h>
+#include <stdarg.h>
 #include <stddef.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -22,6 +23,7 @@
 
 #include "ersd.h"
 #include "ersd_device.cuh"
+#include "ersd_host.h"
 
 namespace ersd {
 
@@ -56,34 +58,18 @@ static thread_local char g_last_launch[192] = "";  // ersd_last_launch(): what t
 
 // The error stays with the library: the runtime keeps it per thread too, where the next check of some
 // other launch on this thread would find it.
-static int cuda_fail(cudaError_t e) {
+int cuda_fail(cudaError_t e) {
   g_last_cuda_error = (int)e;
   (void)cudaGetLastError();
   return ERSD_ECUDA;
 }
 
-// A launch that may start while the kernel before it on the stream still runs (see
-// wait_for_previous_kernel), in clusters of CL blocks.
-struct Launch {
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute at[2];
-  Launch(dim3 grid, unsigned threads, size_t smem, cudaStream_t st, unsigned CL = 1) {
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = CL;
-    at[1].val.clusterDim.y = 1;
-    at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = CL > 1 ? 2 : 1;
-  }
-  Launch(const Launch&) = delete;
-};
+void note_launch(const char* format, ...) {
+  va_list a;
+  va_start(a, format);
+  vsnprintf(g_last_launch, sizeof g_last_launch, format, a);
+  va_end(a);
+}
 
 struct OwnedWorkspace {
   void* ptr = nullptr;
@@ -156,7 +142,7 @@ static bool rows_aligned(const void* base, int64_t ld, int dt) {
 constexpr int kMinChunkTiles = 8;  // smallest chunk of a row that the default split makes
 
 // Multiprocessors of the current device (asked once per device; 148 on a B200).
-static int sm_count() {
+int sm_count() {
   static std::mutex m;
   static int count[64];
   int dev = 0;
