@@ -451,7 +451,8 @@ typedef struct ersd_logit_opts {
   const int32_t* prompt_lens;   /* device [B]: how many of these are the prompt; NULL = 0 */
   const int32_t* draft_tokens;  /* device: chain [B, R-1], entry j = token drafted at position j (row j + 1 follows
                                    it); tree [B, R], entry n = token drafted at node n (entry 0 unused) */
-  const int32_t* parent;        /* HOST [R]: draft tree of the rows; NULL = chain */
+  const int32_t* parent;        /* HOST [R]: draft tree of the rows; NULL = chain; not looked at without
+                                   draft_tokens */
   const float* repetition;      /* device [B]; > 0 */
   const float* presence;        /* device [B] */
   const float* frequency;       /* device [B] */
@@ -484,8 +485,8 @@ typedef struct ersd_logit_opts {
  *   itself with the same row stride (tokens that nothing changes are then neither read nor written)
  * Entries V..ld-1 of a row are left alone.
  * Errors: ERSD_EINVAL (null pointers, sizes < 1, strides below V, draft_tokens or parent that do not
- * go with R, values without tokens, ...); ERSD_EALIGN; ERSD_EUNSUPPORTED for B > 65535, draft tokens
- * with R > ERSD_MAX_ROWS, V > 0x7FFF0000, bias_count > ERSD_MAX_BIASES.
+ * go with R, values without tokens, ...); ERSD_EALIGN; ERSD_EUNSUPPORTED for B or R > 65535, draft
+ * tokens with R > ERSD_MAX_ROWS, V > 2^28, bias_count > ERSD_MAX_BIASES.
  */
 int ersd_process_logits(const void* logits, void* out, ersd_dtype dt, int B, int R, int V, const ersd_logit_opts* opts,
                         void* cuda_stream);

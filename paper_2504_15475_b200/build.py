@@ -10,7 +10,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SRC = [os.path.join(CSRC, name) for name in ("ersd.cu", "ersd_cluster_bf16.cu", "ersd_cluster_f32.cu", "ersd_attention.cu", "ersd_cache.cu",
+SRC = [os.path.join(CSRC, name) for name in ("ersd.cu", "ersd_cluster_bf16.cu", "ersd_cluster_f32.cu", "ersd_attention.cu", "ersd_attention_tensor.cu", "ersd_cache.cu",
                                                    "ersd_logits.cu", "ersd_tree.cpp")]
 DEPS = SRC + [os.path.join(CSRC, name) for name in ("ersd_device.cuh", "ersd_math.cuh", "ersd_kernel.inc", "ersd_cluster.inc",
                                                     "ersd_cluster_top.inc", "ersd_cluster_select.inc", "ersd_gsd.inc", "ersd_host.h",

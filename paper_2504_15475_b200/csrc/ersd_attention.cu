@@ -318,8 +318,7 @@ int launch_attention_f32(AttentionParams& p, bool bf16, int max_context, cudaStr
     p.split = 1;
     while (p.split < 8 && units * p.split < 2 * sm_count() && p.split * 2 <= tiles) p.split *= 2;
   }
-  if (p.split > 8) return ERSD_EUNSUPPORTED;
-  if ((int64_t)p.row_tiles * p.split > 0x7FFFFFFF) return ERSD_EUNSUPPORTED;
+  if (p.split > 8) p.split = 8;
   cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem);
   if (e != cudaSuccess) return cuda_fail(e);
   note_launch("attention_kernel<%s, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows", bf16 ? "bf16" : "f32", k.rows, kThreads,
@@ -400,6 +399,10 @@ extern "C" int ersd_chunk_attention(const ersd_cache* cache, const void* q, void
   int max_context = o.max_context;
   if (!max_context || max_context > p.capacity) max_context = p.capacity;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (o.kernel_path == 2) return ERSD_EUNSUPPORTED;
+  if (o.kernel_path != 1) {
+    const int status = c.dtype == ERSD_BF16 ? launch_attention_tensor(p, max_context, st) : ERSD_EUNSUPPORTED;
+    if (status != ERSD_EUNSUPPORTED || o.kernel_path == 2) return status;
+    p.split = o.split;
+  }
   return launch_attention_f32(p, c.dtype == ERSD_BF16, max_context, st);
 }

@@ -1,0 +1,730 @@
+// ersd_chunk_attention on tensor cores: bfloat16 caches with heads of 64 or 128.
+//
+// A thread block takes 128 or 256 packed rows of one kv head (see AttentionParams) through its keys, 128 slots at
+// a time.  One warp copies keys and values page by page with TMA into a ring of shared memory, one thread issues
+// the products (tcgen05.mma), and two groups of four warps do the softmax, a thread to a row: scores come out of
+// tensor memory, weights go back there as bfloat16 over the scores they came from, and the second product takes
+// them from there.  The two groups work on two independent streams, so that one's products run while the other's
+// softmax does: with 256 rows a stream is half of the rows; with up to 128, where the cache's bytes bound the
+// call, both streams have the same rows and take turns at the tiles of keys, and are joined at the end.
+//
+// The output's accumulator stays in tensor memory.  It is scaled only when a row's maximum has risen by more than
+// 2^8 since the last time (weights are then at most 2^8, which bfloat16 and the 32-bit sums hold as well as 1);
+// the end divides by a sum formed with the same maximum, so this changes no result beyond rounding.
+//
+// `split` blocks of a cluster share the keys and join their outputs through distributed shared memory.
+#include <cooperative_groups.h>
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include <mutex>
+
+#include "ersd_attention.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace ersd {
+
+namespace {
+
+constexpr int kN = 128;               // slots of a tile of keys
+constexpr int kSoftmaxThreads = 256;  // two groups of four warps
+constexpr int kTensorThreads = kSoftmaxThreads + 64;
+constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before its output is scaled
+
+template <int D, int NT>
+struct Plan {
+  static constexpr int kStageBytes = kN * D * 2;                                   // keys or values of a tile
+  static constexpr int kStages = D == 64 ? 12 : NT == 1 ? 6 : 5;
+  static constexpr int kQBytes = NT * 128 * D * 2;
+  static constexpr int kRows = NT * 128;
+  // (the largest is all that a block may have; every one is more than half of it, so that no two blocks, each
+  // with all of the tensor memory, ever meet on an SM)
+  static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes + 1024;
+  static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
+  static_assert(kRows * (kPartRow + 2) * 4 <= kStages * kStageBytes, "");
+  static_assert(kSmem <= 232448 && kSmem > 120000, "");
+};
+
+struct Misc {  // behind the ring
+  uint64_t full[12], empty[12];  // of the ring's stages
+  uint64_t scores[2];            // a stream's scores are in tensor memory
+  uint64_t weights[2];           // and its weights, instead of them
+  uint64_t done;                 // all products
+  uint32_t tmem;
+  uint32_t gave_up;              // a wait ran out: nothing that follows it can be trusted
+  uint8_t parent[ERSD_MAX_ROWS], depth[ERSD_MAX_ROWS];
+};
+static_assert(sizeof(Misc) <= 1024, "");
+
+__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint64_t* b, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_address(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_address(b)) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_address(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_address(b)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Whether the phase ended; false when it did not within some seconds, or another wait of the block ran out.
+__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, uint32_t* gave_up) {
+  if (barrier_try(b, parity)) return true;
+  for (int i = 0; i < (1 << 22); ++i) {
+    if (barrier_try(b, parity)) return true;
+    if (*(volatile uint32_t*)gave_up) return false;
+  }
+  *(volatile uint32_t*)gave_up = 1;
+  return false;
+}
+
+__device__ __forceinline__ void tma_box(uint32_t to, const CUtensorMap* map, int x, int token, int head, int page, uint64_t* full) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+      "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(smem_address(full))
+      : "memory");
+}
+
+// Descriptor of an operand in shared memory, in rows of 128 bytes with their 16-byte pieces swizzled in groups of
+// eight rows (1024 bytes apart); `lead`: bytes between panels of 64 elements along the row where the rows run
+// along the operand's outer dimension.
+__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t lead) {
+  return (uint64_t)((address & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Instruction descriptor: bfloat16 times bfloat16 into 32 bits, 128 x n; `outer`: B's rows run along n.
+__host__ __device__ constexpr uint32_t instruction(int n, bool outer) {
+  return 1u << 4 | 1u << 7 | 1u << 10 | (outer ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+}
+__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_address(b)) : "memory");
+}
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+#define R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
+#define S8(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3]), "r"(a[i + 4]), "r"(a[i + 5]), "r"(a[i + 6]), "r"(a[i + 7])
+// 32 columns of this warp's 32 rows of tensor memory
+__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24)
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::S8(r, 0),
+      S8(r, 8), S8(r, 16), S8(r, 24), "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float power_of_two(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pair(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+
+// Bits [a, b) of a word, both cut to 0..32.
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+  a = max(a, 0);
+  b = min(b, 32);
+  if (a >= b) return 0u;
+  return (0xFFFFFFFFu >> (32 - (b - a))) << a;
+}
+
+// The order in which the ring is filled is the order of use.  Step u of the products is tile tile_of(u) for stream
+// u & 1; with 256 rows both streams use every tile (NT = 2: steps 2t and 2t + 1), else a tile has one step.
+// Items: the keys of the first tiles, then by step its values and the keys of that stream's next tile.
+template <int NT>
+struct Order {
+  int tiles;
+  __device__ __forceinline__ int items() const { return 2 * tiles; }
+  __device__ __forceinline__ int keys_of(int t) const {
+    if (NT == 2) return 2 * t;
+    return t < 2 ? t : min(tiles, 2) + 2 * (t - 2) + 1;
+  }
+  __device__ __forceinline__ int values_of(int t) const {
+    if (NT == 2) return 2 * t + 1;
+    return min(tiles, 2) + t + min(t, max(tiles - 2, 0));
+  }
+  // item q: its tile; whether it is values
+  __device__ __forceinline__ int tile(int q, bool* values) const {
+    if (NT == 2) {
+      *values = q & 1;
+      return q >> 1;
+    }
+    const int first = min(tiles, 2);
+    *values = false;
+    if (q < first) return q;
+    const int x = q - first, both = 2 * max(tiles - 2, 0);  // values 0, keys 2, values 1, keys 3, ...
+    if (x < both) {
+      *values = !(x & 1);
+      return (x >> 1) + (x & 1) * 2;
+    }
+    *values = true;
+    return (both >> 1) + x - both;
+  }
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kTensorThreads, 1)
+    attention_tensor_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map,
+                            const __grid_constant__ CUtensorMap v_map, const int box) {
+  using P = Plan<D, NT>;
+  constexpr int kStages = P::kStages, kPanel = kN * 128;  // bytes of a panel: 128 rows of 64 elements
+  extern __shared__ char raw[];
+  char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  char* q_tile = base;
+  char* ring = base + P::kQBytes;
+  Misc& sh = *(Misc*)(ring + kStages * P::kStageBytes);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int kv_head = blockIdx.y, b = blockIdx.z;
+  const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
+
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int rows = p.row_counts ? p.row_counts[b] : p.R;
+  rows = max(0, min(rows, p.R));
+  const int m0 = tile * P::kRows, m1 = min(m0 + P::kRows, rows * p.group);
+  if (m0 >= m1) return;  // (the same for every block of the cluster)
+  const int ctx = max(0, p.context_lens[b]);
+  const int r0 = m0 / p.group, r1 = (m1 - 1) / p.group + 1;
+  // warps of each stream with rows
+  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = NT == 1 ? warps0 : (max(m1 - m0 - 128, 0) + 31) / 32;
+  int min_depth = r0;
+  if (p.tree) {
+    min_depth = p.depth[r0];
+    for (int r = r0 + 1; r < r1; ++r) min_depth = min(min_depth, (int)p.depth[r]);
+  }
+  const KeyRange keys = key_range<kN>(p, ctx, r1, min_depth);
+  const int t0 = (int)((int64_t)keys.tiles * part / p.split), t1 = (int)((int64_t)keys.tiles * (part + 1) / p.split);
+  const Order<NT> order{t1 - t0};
+  const int tiles = t1 - t0;
+
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(&sh.full[i], 1);
+      barrier_init(&sh.empty[i], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      barrier_init(&sh.scores[s], 1);
+      barrier_init(&sh.weights[s], (uint32_t)max(1, s ? warps1 : warps0));
+    }
+    barrier_init(&sh.done, 1);
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_address(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (p.tree)
+    for (int n = tid; n < ERSD_MAX_ROWS; n += kTensorThreads) {
+      sh.parent[n] = p.parent[n];
+      sh.depth[n] = p.depth[n];
+    }
+  if (tid < kSoftmaxThreads) {
+    // the rows of q in the operand's layout; rows that are not there stay as they are: their scores go nowhere
+    const __nv_bfloat16* q = (const __nv_bfloat16*)p.q + b * p.q_b;
+    const bool wide = ((p.q_b | p.q_r | p.q_h) & 7) == 0 && ((uintptr_t)p.q & 15) == 0;
+    const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the softmax takes a positive scale)
+    constexpr int kPieces = D / 8;
+    for (int i = tid; i < (m1 - m0) * kPieces; i += kSoftmaxThreads) {
+      const int m = i / kPieces, c = i % kPieces, r = (m0 + m) / p.group, g = m0 + m - r * p.group;
+      const __nv_bfloat16* at = q + r * p.q_r + (kv_head * p.group + g) * p.q_h + c * 8;
+      uint4 x;
+      if (wide) {
+        x = *(const uint4*)at;
+      } else {
+        const unsigned short* e = (const unsigned short*)at;
+        x = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+      }
+      x.x ^= flip;
+      x.y ^= flip;
+      x.z ^= flip;
+      x.w ^= flip;
+      const int row = m & 127;
+      *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = sh.tmem;
+  uint32_t* const gave_up = &sh.gave_up;
+
+  float top = -INFINITY, sum = 0.f;  // of the row of a softmax thread: the maximum its weights were formed with, their sum
+  if (warp == 8) {
+    // ---- copies: a lane has one box (`box` slots by 64 elements) of every item
+    const int boxes = kN / box, group = lane % boxes, panel = lane / boxes;
+    const bool mine = panel < D / 64;
+    const int32_t* table = p.table + b * p.table_stride;
+    auto entry = [&](int q, bool* needed) {  // page of this lane's box of item q
+      bool values;
+      *needed = false;
+      if (!mine || q >= order.items()) return 0;
+      const int slot = tile_start<kN>(keys, t0 + order.tile(q, &values)) + group * box;
+      *needed = slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo);
+      return *needed ? table[slot / p.page_size] : 0;
+    };
+    constexpr int kAhead = 4;  // items whose table entries are asked for early
+    int page[kAhead];
+    bool needed[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) page[j] = entry(j, &needed[j]);
+    int q = 0;
+    for (; q < order.items(); ++q) {
+      const int stage = q % kStages;
+      const int page_now = page[0];
+      const bool needed_now = needed[0];
+#pragma unroll
+      for (int j = 0; j + 1 < kAhead; ++j) {
+        page[j] = page[j + 1];
+        needed[j] = needed[j + 1];
+      }
+      page[kAhead - 1] = entry(q + kAhead, &needed[kAhead - 1]);
+      if (q >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], (uint32_t)(q / kStages - 1) & 1, gave_up))) break;
+      bool values;
+      const int slot = tile_start<kN>(keys, t0 + order.tile(q, &values)) + group * box;
+      const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, needed_now));
+      if (lane == 0) barrier_expect(&sh.full[stage], count * (uint32_t)box * 128u);
+      __syncwarp();
+      // (page numbers outside the cache give zeros)
+      if (needed_now)
+        tma_box(smem_address(ring + stage * P::kStageBytes + panel * kPanel + group * box * 128), values ? &v_map : &k_map, panel * 64,
+                slot % p.page_size, kv_head, page_now < 0 || page_now >= p.num_pages ? p.num_pages : page_now, &sh.full[stage]);
+      __syncwarp();
+    }
+    // every copy has landed before the block ends, even where the products gave up
+    if (*(volatile uint32_t*)gave_up)
+      for (int x = max(0, q - kStages); x < q; ++x)
+        for (int i = 0; i < (1 << 22) && !barrier_try(&sh.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
+        }
+  } else if (warp == 9) {
+    // ---- products
+    if (lane == 0 && tiles > 0) {
+      constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
+      const int steps = NT == 2 ? 2 * tiles : tiles;
+      const bool second = NT == 2 ? warps1 > 0 : tiles > 1;  // whether stream 1 has anything
+      bool ok = true;
+      auto wait_item = [&](int q) { return barrier_wait(&sh.full[q % kStages], (uint32_t)(q / kStages) & 1, gave_up); };
+      auto score = [&](int s, int t) {  // scores of stream s with tile t
+        const int item = order.keys_of(t);
+        if (!wait_item(item)) return false;
+        after_sync();
+        const uint32_t a = smem_address(q_tile) + (NT == 2 ? s * 128 * D * 2 : 0), k = smem_address(ring + (item % kStages) * P::kStageBytes);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          const uint32_t at = (j >> 2) * kPanel + (j & 3) * 32;
+          mma_shared(tmem + s * kN, operand(a + at, 16), operand(k + at, 16), kScores, j > 0);
+        }
+        mma_commit(&sh.scores[s]);
+        if (NT == 1 || s == 1 || !second) mma_commit(&sh.empty[item % kStages]);
+        return true;
+      };
+      ok = score(0, 0);
+      if (ok && second) ok = score(1, NT == 2 ? 0 : 1);
+      for (int u = 0; ok && u < steps; ++u) {
+        const int s = u & 1, i = u >> 1, t = NT == 2 ? i : u;
+        if (s == 1 && !second) continue;
+        if (!barrier_wait(&sh.weights[s], (uint32_t)i & 1, gave_up)) break;
+        const int item = order.values_of(t);
+        if (!wait_item(item)) break;
+        after_sync();
+        const uint32_t v = smem_address(ring + (item % kStages) * P::kStageBytes);
+#pragma unroll
+        for (int j = 0; j < kN / 16; ++j)
+          mma_tmem(tmem + 2 * kN + s * D, tmem + s * kN + j * 8, operand(v + j * 16 * 128, kPanel), kOutput, i > 0 || j > 0);
+        if (NT == 1 || s == 1 || !second) mma_commit(&sh.empty[item % kStages]);
+        const int next = NT == 2 ? t + 1 : t + 2;
+        if (next < tiles) ok = score(s, next);
+      }
+      mma_commit(&sh.done);
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax: a thread has one row
+    const int s = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane, m = m0 + (NT == 2 ? s * 128 : 0) + row;
+    const int my_warps = s ? warps1 : warps0;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t scores = tmem + lanes + s * kN, output = tmem + lanes + 2 * kN + s * D;
+    const int mine = NT == 2 ? tiles : s ? tiles / 2 : (tiles + 1) / 2;
+    if (quarter < my_warps) {
+      const float scale = fabsf(p.scale_log2);
+      const int r = min(m, m1 - 1) / p.group;  // (rows of a warp behind the last: as the last, and not written)
+      const int depth = p.tree ? (int)sh.depth[r] : r;
+      const int lo = p.window ? max(0, ctx + depth - p.window + 1) : 0;   // cached slots from lo on, and below `sinks`
+      const int hi = min(keys.hi, p.tree ? ctx : ctx + r + 1);
+      const int sinks = p.window ? min(p.sinks, hi) : 0;
+      // what the first and the last row of the stream see of the cache bounds the tiles that need no mask
+      const int first_m = m0 + (NT == 2 ? s * 128 : 0), last_m = min(first_m + 128, m1) - 1;
+      const int all_hi = min(keys.hi, p.tree ? ctx : ctx + first_m / p.group + 1);
+      const int all_lo = p.window ? ctx + (p.tree ? p.R - 1 : last_m / p.group) - p.window + 1 : 0;
+      for (int i = 0; i < mine; ++i) {
+        const int t = NT == 2 ? i : 2 * i + s;
+        const int start = tile_start<kN>(keys, t0 + t);
+        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.scores[s], (uint32_t)i & 1, gave_up))) break;
+        after_sync();
+        uint32_t x[kN];
+#pragma unroll
+        for (int c = 0; c < kN; c += 32) tmem_load(scores + c, x + c);
+        tmem_loaded();
+        const bool whole = start + kN <= all_hi && (start >= all_lo || start + kN <= p.sinks);
+        if (!whole) {
+          uint32_t see[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int at = start + 32 * w;
+            see[w] = bits_between(lo - at, hi - at) | bits_between(-at, sinks - at);
+          }
+          if (p.tree) {
+            for (int n = r;; n = sh.parent[n]) {
+              const int pos = ctx + (int)sh.depth[n], at = ctx + n - start;
+              if (at >= 0 && at < kN && ctx + n < keys.hi && (!p.window || pos >= lo || pos < p.sinks)) {
+                const uint32_t bit = 1u << (at & 31);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) see[w] |= (at >> 5) == w ? bit : 0u;
+              }
+              if (n == 0) break;
+            }
+            __syncwarp();
+          }
+#pragma unroll
+          for (int c = 0; c < kN; ++c) x[c] = see[c >> 5] >> (c & 31) & 1u ? x[c] : 0xFF800000u;
+          // Values of slots that no row of the block sees are whatever was there: 0 * NaN is no 0.  (Both streams
+          // may write the same zeros.)
+          bool any_dead = keys.dead(start) || keys.dead(start + kN - 1);
+          if (!any_dead) any_dead = keys.sink_hi < keys.lo && keys.sink_hi < start + kN && keys.lo > start;
+          if (any_dead) {
+            const int item = order.values_of(t);
+            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.full[item % kStages], (uint32_t)(item / kStages) & 1, gave_up))) break;
+            // the stream's warps share the tile's rows
+            for (int n = row; n < kN; n += my_warps * 32)
+              if (keys.dead(start + n)) {
+                char* v = ring + (item % kStages) * P::kStageBytes + n * 128;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) *(uint4*)(v + c * kPanel + j * 16) = make_uint4(0, 0, 0, 0);
+              }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+        }
+        float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kN; c += 4)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[j] = fmaxf(a[j], __uint_as_float(x[c + j]));
+        const float now = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * scale;
+        const bool rise = now > top + kRise;  // (also from nothing seen to something)
+        if (i == 0) {
+          top = now;
+        } else if (__any_sync(0xFFFFFFFFu, rise)) {
+          // (the scores of this tile come after the product with the last weights: the output is at rest)
+          const float f = rise ? power_of_two(top - now) : 1.0f;
+          sum *= f;
+          if (rise) top = now;
+#pragma unroll
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_load(output + c, o);
+            tmem_loaded();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_store(output + c, o);
+          }
+        }
+        const float minus = top == -INFINITY ? 0.f : -top;
+        float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t w[32];
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            const float e0 = power_of_two(fmaf(__uint_as_float(x[half * 64 + c]), scale, minus));
+            const float e1 = power_of_two(fmaf(__uint_as_float(x[half * 64 + c + 1]), scale, minus));
+            part_sum[c & 2] += e0;
+            part_sum[(c & 2) + 1] += e1;
+            w[c >> 1] = pair(e0, e1);
+          }
+          tmem_store(scores + half * 32, w);
+        }
+        sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+        tmem_stored();
+        before_sync();
+        __syncwarp();
+        if (lane == 0) barrier_arrive(&sh.weights[s]);
+      }
+    }
+  }
+
+  // ---- the end: every product is done, the ring is free
+  if (tiles > 0) {
+    // (asked for in every case: after a wait that ran out, products may still be under way)
+    for (int i = 0; i < (1 << 22) && !barrier_try(&sh.done, 0); ++i) {
+    }
+    __syncwarp();
+    after_sync();
+  }
+  if (warp < 8) {
+    const int s = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t output = tmem + ((uint32_t)(quarter * 32) << 16) + 2 * kN + s * D;
+    const int mine = NT == 2 ? tiles : s ? tiles / 2 : (tiles + 1) / 2;
+    const bool there = quarter < (s ? warps1 : warps0);
+    float* parts = (float*)ring;                         // [rows][kPartRow]
+    float* tops = parts + P::kRows * P::kPartRow;        // [rows]
+    float* sums = tops + P::kRows;                       // [rows]
+    const int m = m0 + (NT == 2 ? s * 128 : 0) + row;
+    float o[D];
+    if (there && mine > 0) {
+#pragma unroll
+      for (int c = 0; c < D; c += 32) tmem_load(output + c, (uint32_t*)o + c);
+      tmem_loaded();
+    } else {
+#pragma unroll
+      for (int c = 0; c < D; ++c) o[c] = 0.f;
+      top = -INFINITY;
+      sum = 0.f;
+    }
+    if (*(volatile uint32_t*)gave_up) sum = __uint_as_float(0x7FC00000u);  // NaN: seen by whoever reads the output
+    auto keep = [&]() {
+      const int at = NT == 2 ? s * 128 + row : row;
+#pragma unroll
+      for (int c = 0; c < D; c += 4) *(float4*)(parts + at * P::kPartRow + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+      tops[at] = top;
+      sums[at] = sum;
+    };
+    if (NT == 1) {
+      if (s == 1 && there) keep();
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (s == 0 && there && sums[row] != 0.f) {
+        const float other = tops[row], now = fmaxf(top, other), at = now == -INFINITY ? 0.f : now;
+        const float f = power_of_two(top - at), g = power_of_two(other - at);
+#pragma unroll
+        for (int c = 0; c < D; c += 4) {
+          const float4 x = *(const float4*)(parts + row * P::kPartRow + c);
+          o[c] = o[c] * f + x.x * g;
+          o[c + 1] = o[c + 1] * f + x.y * g;
+          o[c + 2] = o[c + 2] * f + x.z * g;
+          o[c + 3] = o[c + 3] * f + x.w * g;
+        }
+        sum = sum * f + sums[row] * g;
+        top = now;
+      }
+    }
+    const bool holds = there && (NT == 2 || s == 0);
+    const bool wide = ((p.o_b | p.o_r | p.o_h) & 7) == 0 && ((uintptr_t)p.out & 15) == 0;
+    __nv_bfloat16* out = (__nv_bfloat16*)p.out + b * p.o_b;
+    if (p.split == 1) {
+      if (holds && m < m1) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int r = m / p.group, g = m - r * p.group;
+        __nv_bfloat16* at = out + r * p.o_r + (kv_head * p.group + g) * p.o_h;
+#pragma unroll
+        for (int c = 0; c < D; c += 8) {
+          const uint4 x = make_uint4(pair(o[c] * inv, o[c + 1] * inv), pair(o[c + 2] * inv, o[c + 3] * inv),
+                                     pair(o[c + 4] * inv, o[c + 5] * inv), pair(o[c + 6] * inv, o[c + 7] * inv));
+          if (wide) {
+            *(uint4*)(at + c) = x;
+          } else {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ((unsigned short*)at)[c + j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+          }
+        }
+      }
+    } else {
+      if (holds) keep();
+    }
+  }
+  if (p.split > 1) {
+    cg::cluster_group cluster = cg::this_cluster();
+    __syncwarp();
+    cluster.sync();
+    // Join the blocks' outputs: out = sum_c 2^(top_c - top) o_c / sum_c 2^(top_c - top) sum_c.  Rows are dealt out
+    // over the blocks, a thread joins four columns.
+    float* parts = (float*)ring;
+    float* tops = parts + P::kRows * P::kPartRow;
+    float* sums = tops + P::kRows;
+    constexpr int kD4 = D / 4;
+    const bool wide = ((p.o_b | p.o_r | p.o_h) & 3) == 0 && ((uintptr_t)p.out & 7) == 0;
+    for (int i = tid + part * kTensorThreads; i < (m1 - m0) * kD4; i += kTensorThreads * p.split) {
+      const int row = i / kD4, d = (i - row * kD4) * 4;
+      float most = -INFINITY;
+      for (int c = 0; c < p.split; ++c) most = fmaxf(most, *cluster.map_shared_rank(&tops[row], c));
+      if (most == -INFINITY) most = 0.f;
+      float total = 0.f;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < p.split; ++c) {
+        const float theirs = *cluster.map_shared_rank(&sums[row], c);
+        if (theirs == 0.f) continue;
+        const float f = power_of_two(*cluster.map_shared_rank(&tops[row], c) - most);
+        const float4 x = *(const float4*)cluster.map_shared_rank(&parts[row * P::kPartRow + d], c);
+        total = fmaf(f, theirs, total);
+        y.x = fmaf(f, x.x, y.x);
+        y.y = fmaf(f, x.y, y.y);
+        y.z = fmaf(f, x.z, y.z);
+        y.w = fmaf(f, x.w, y.w);
+      }
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      const int r = (m0 + row) / p.group, g = m0 + row - r * p.group;
+      __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h + d;
+      const uint2 x = make_uint2(pair(y.x * inv, y.y * inv), pair(y.z * inv, y.w * inv));
+      if (wide) {
+        *(uint2*)at = x;
+      } else {
+        const uint32_t w[2] = {x.x, x.y};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ((unsigned short*)at)[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+      }
+    }
+    __syncwarp();
+    cluster.sync();  // (no block ends while another reads its shared memory)
+  }
+  before_sync();
+  __syncthreads();
+  if (warp == 9) {
+    after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- host side
+using Encode = decltype(&cuTensorMapEncodeTiled);
+
+Encode encode_function() {
+  static Encode f = [] {
+    void* at = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &at, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      at = nullptr;
+    }
+    return (Encode)at;
+  }();
+  return f;
+}
+
+// The map of one side of the cache: [pages, heads, positions of a page, D], boxes of `box` positions by 64 elements.
+bool encode(CUtensorMap* map, const void* at, int D, const AttentionParams& p, int64_t token, int64_t head, int64_t page, int box) {
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)p.page_size, (cuuint64_t)p.heads, (cuuint64_t)p.num_pages};
+  // (the stride of a dimension of one is free: the map wants a multiple of 16 bytes all the same)
+  if (p.heads == 1) head = D;
+  if (p.num_pages == 1) page = D;
+  if (token <= 0 || head <= 0 || page <= 0 || ((token | head | page) & 7) || !aligned_to(at, 16)) return false;
+  const cuuint64_t strides[3] = {(cuuint64_t)token * 2, (cuuint64_t)head * 2, (cuuint64_t)page * 2};
+  const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
+  for (const cuuint64_t s : strides)
+    if (s >= (cuuint64_t)1 << 40) return false;
+  return encode_function()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(at), dims, strides, boxes, steps,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct TensorBuild {
+  const void* kernel;
+  int smem, rows;
+};
+template <int D, int NT>
+TensorBuild tensor_build() {
+  return {(const void*)attention_tensor_kernel<D, NT>, Plan<D, NT>::kSmem, Plan<D, NT>::kRows};
+}
+
+// What a build needs before its first launch on a device; the largest cluster it can be launched in.
+int prepare_build(const TensorBuild& k, int at, int* limit) {
+  static std::mutex m;
+  static int known[4][64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e);
+  if (dev < 0 || dev >= 64) return ERSD_EUNSUPPORTED;
+  std::lock_guard<std::mutex> lock(m);
+  if (!known[at][dev]) {
+    e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
+    if (e != cudaSuccess) return cuda_fail(e);
+    int n = 0;
+    e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) {
+      Launch l(dim3(16, 1, 1), kTensorThreads, (size_t)k.smem, nullptr, 16);
+      l.cfg.attrs = &l.at[1];  // (the cluster's size alone)
+      l.cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&n, k.kernel, &l.cfg);
+    }
+    (void)cudaGetLastError();  // a refused opt-in only means clusters of eight
+    known[at][dev] = e == cudaSuccess && n >= 1 ? 16 : 8;
+  }
+  *limit = known[at][dev];
+  return ERSD_OK;
+}
+
+}  // namespace
+
+int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st) {
+  if ((p.dim != 64 && p.dim != 128) || p.page_size % 8 || !encode_function()) return ERSD_EUNSUPPORTED;
+  int box = 8;
+  while (box < 128 && p.page_size % (box * 2) == 0) box *= 2;
+  CUtensorMap k_map, v_map;
+  if (!encode(&k_map, p.k, p.dim, p, p.k_token, p.k_head, p.k_page, box) || !encode(&v_map, p.v, p.dim, p, p.v_token, p.v_head, p.v_page, box))
+    return ERSD_EUNSUPPORTED;
+  const int two = (int64_t)p.R * p.group > 128;
+  const TensorBuild k = p.dim == 64 ? (two ? tensor_build<64, 2>() : tensor_build<64, 1>()) : (two ? tensor_build<128, 2>() : tensor_build<128, 1>());
+  int limit = 8;
+  const int status = prepare_build(k, (p.dim == 64 ? 0 : 2) + two, &limit);
+  if (status != ERSD_OK) return status;
+  p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
+  if (!p.split) {
+    // as many blocks as SMs, with a tile of keys at least for each
+    const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
+    int64_t reach = (int64_t)max_context + p.R;
+    if (p.window && reach > (int64_t)p.window + p.sinks + p.R) reach = (int64_t)p.window + p.sinks + p.R;
+    const int64_t tiles = (reach + kN - 1) / kN;
+    p.split = 1;
+    while (p.split < limit && units * p.split * 2 <= sm_count() && p.split * 2 <= tiles) p.split *= 2;
+  }
+  if (p.split > limit) p.split = limit;
+  note_launch("attention_tensor_kernel<%d, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows, boxes of %d", p.dim, k.rows,
+              kTensorThreads, p.row_tiles * p.split, p.heads, p.B, p.split, box);
+  Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), kTensorThreads, (size_t)k.smem, st, (unsigned)p.split);
+  void* args[] = {(void*)&p, (void*)&k_map, (void*)&v_map, (void*)&box};
+  const cudaError_t e = cudaLaunchKernelExC(&l.cfg, k.kernel, args);
+  return e == cudaSuccess ? ERSD_OK : cuda_fail(e);
+}
+
+}  // namespace ersd

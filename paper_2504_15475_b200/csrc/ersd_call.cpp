@@ -536,8 +536,7 @@ PyObject* process_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
       o.prompt_lens = small<int32_t>(a[4], {B}, x, "prompt_lens");
     }
     std::vector<int32_t> parent;
-    if (a[6] != Py_None) {
-      if (a[5] == Py_None) refuse(PyExc_ValueError, "%s needs draft_tokens", "parent");
+    if (a[6] != Py_None && a[5] != Py_None) {
       parent = parents(a[6], (int)R);
       o.parent = parent.data();
     }

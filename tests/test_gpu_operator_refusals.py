@@ -53,7 +53,7 @@ def test_logits(ersd):
     i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
     f = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
     for kw in (dict(history=i(3, 4)), dict(history=i(2, 4).long()), dict(history=i(2, 4), history_lens=i(3)), dict(draft_tokens=i(2, 3)),
-               dict(draft_tokens=i(2, 2), parent=[-1, 0, 0]), dict(parent=[-1, 0, 0]), dict(repetition=f(3)), dict(presence=f(2).double()),
+               dict(draft_tokens=i(2, 2), parent=[-1, 0, 0]), dict(repetition=f(3)), dict(presence=f(2).double()),
                dict(bias_tokens=i(2, 4)), dict(bias_tokens=i(2, 4), bias_values=f(2, 5)), dict(bias_tokens=i(3, 4), bias_values=f(3, 4)),
                dict(mask=i(2, 3, 3)), dict(mask=i(2, 2, 4)), dict(mask=i(2, 4)), dict(V=101), dict(V=0), dict(mask=i(2, 3, 8)[..., ::2])):
         with pytest.raises((ValueError, TypeError)):

@@ -141,7 +141,7 @@ def test_logits(L):
                         (dict(history_lens=P), EINVAL), (dict(prompt_lens=P), EINVAL), (dict(history=P, history_width=-1), EINVAL),
                         (dict(bias_tokens=P), EINVAL), (dict(bias_values=P), EINVAL), (dict(bias_count=1, bias_tokens=P), EINVAL),
                         (dict(bias_count=-1), EINVAL), (dict(bias_count=1, bias_tokens=P, bias_values=P, bias_stride=-1), EINVAL),
-                        (dict(mask=P, mask_stride_b=-1), EINVAL), (dict(mask=P, mask_stride_r=-1), EINVAL), (dict(parent=P), EINVAL),
+                        (dict(mask=P, mask_stride_b=-1), EINVAL), (dict(mask=P, mask_stride_r=-1), EINVAL),
                         (dict(history=P + 2, history_width=4), EALIGN), (dict(mask=P + 1), EALIGN), (dict(repetition=P + 2), EALIGN),
                         (dict(bias_count=65536, bias_tokens=P, bias_values=P), EUNSUP)]:
         assert call(o=opts(LogitOpts, **bad)) == status, bad
