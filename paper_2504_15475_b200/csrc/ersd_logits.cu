@@ -2,12 +2,11 @@
 //
 // Bytes bound the operator: every row is read and written once.  Few tokens are changed by more than the mask,
 // and which ones is the same for all rows of a sequence, up to the drafted tokens on a row's path.  So one block
-// takes a slice of the vocabulary for ALL rows of a sequence.  It copies the slice of every row, with -inf where
-// the mask forbids a token (eight tokens that are all forbidden are not read), counts the history's tokens that
-// fall into the slice in shared memory (integers: no order of the atomics changes a result), lists the tokens
-// that occur, and writes those of every row again, each from its own logit.  Changing them while copying would
-// cost a warp the work for every token that any of its 256 is listed for: 303 us instead of 62 for 64 sequences
-// of nine rows with histories of 3000 tokens.
+// takes a slice of the vocabulary for ALL rows of a sequence, and each of its warps a chunk of kChunk tokens: bulk
+// copies bring the chunk of one row after the other into a ring of shared memory while the block counts the
+// history's tokens that fall into its slice (integers: no order of the atomics changes a result) and lists those
+// that occur; the warp changes the listed tokens and the masked ones in shared memory, and a bulk copy takes the
+// chunk away.  A chunk of which the mask allows nothing is not read.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -17,20 +16,29 @@ namespace ersd {
 
 namespace {
 
-constexpr int kGroup = 8;            // consecutive tokens a thread takes at a time
-constexpr int kAhead = 4;            // groups whose loads a thread issues before it works on the first
-constexpr int kLogitThreads = 512;
-constexpr uint32_t kSeen = 1u << 31;     // in the history
-constexpr uint32_t kDrafted = 1u << 30;  // among the sequence's drafted tokens: its count depends on the row
-constexpr uint32_t kBiased = 1u << 29;
-constexpr uint32_t kCount = kBiased - 1;
+constexpr int kChunk = 1024;          // tokens of a warp's chunk: 32 to a lane
+constexpr int kRing = 4;              // rows of a chunk in shared memory
+constexpr int kLogitWarps = 4;        // that have a chunk; as many more help to count the history
+constexpr int kLogitThreads = 2 * 32 * kLogitWarps;
+constexpr int kMaskRing = 8;          // rows of its mask
+constexpr int kSlice = kLogitWarps * kChunk;
+constexpr int kLead = 8;              // most tokens a row's chunks start before the slice: see below
+constexpr int kSpan = kSlice + kLead;
+constexpr int kLists = kLogitWarps + 1;
+// An entry of the table: how often the token occurs behind the prompt, and
+constexpr uint32_t kSeen = 1u << 31;     // that it is in the history
+constexpr uint32_t kDrafted = 1u << 30;  // that it is among the drafted tokens: its count depends on the row
+constexpr uint32_t kBiased = 1u << 29;   // that it has a bias, whose index + 1 is here where the history is short ...
+constexpr int kBiasShift = 13;
+constexpr uint32_t kShortCount = (1u << kBiasShift) - 1, kLongCount = kBiased - 1;  // ... and else in a table of its own
 
 struct LogitParams {
   const void* in;
   void* out;
   int64_t ld_in, ld_out;
-  int B, R, V, slice;
+  int B, R, V;
   int in_place;
+  int long_history;  // counts may need more than kShortCount
   const int32_t *history, *history_lens, *prompt_lens, *draft_tokens;
   int history_width, tree;
   const float *repetition, *presence, *frequency;
@@ -56,182 +64,313 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// Eight bits from bit position `at` on of a bitmap whose words past `last` do not exist.
-__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int at, int last) {
-  const int w = at >> 5;
-  const uint32_t lo = words[w], hi = (at & 31) > 24 && w < last ? words[w + 1] : 0u;
-  return __funnelshift_r(lo, hi, at & 31) & 0xFFu;
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// Four bytes to shared memory without a register that waits for them; zeros where `there` is false.
+__device__ __forceinline__ void copy_word(uint32_t* to, const uint32_t* from, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(to)), "l"(from), "r"(there ? 4 : 0) : "memory");
+}
+// The top bit of `hi` in all bits of the upper half, that of `lo` in all of the lower.
+__device__ __forceinline__ uint32_t spread_tops(uint32_t hi, uint32_t lo) {
+  uint32_t d;
+  asm("prmt.b32 %0, %1, %2, 0xBBFF;" : "=r"(d) : "r"(hi), "r"(lo));
+  return d;
+}
+__device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* full) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_address(to)),
+               "l"(from), "r"(bytes), "r"(shared_address(full))
+               : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* to, const void* from, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(shared_address(from)), "r"(bytes) : "memory");
 }
 
 template <typename T>
-struct alignas(16) Group {
-  static constexpr int kWords = kGroup * (int)sizeof(T) / 4;
-  uint32_t w[kWords];
-  __device__ __forceinline__ void forbid(uint32_t allow) {  // -inf where a bit is 0
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) {
-      if constexpr (sizeof(T) == 4) {
-        if (!(allow >> j & 1u)) w[j] = 0xFF800000u;
-      } else {
-        if (!(allow >> (2 * j) & 1u)) w[j] = (w[j] & 0xFFFF0000u) | 0xFF80u;
-        if (!(allow >> (2 * j) & 2u)) w[j] = (w[j] & 0xFFFFu) | 0xFF800000u;
-      }
-    }
-  }
+struct LogitShared {
+  T ring[kLogitWarps][kRing][kChunk];
+  uint64_t full[kLogitWarps][kRing];
+  uint32_t table[kSpan];             // counts and flags of the slice's tokens
+  uint32_t touched[kLists][32];      // by chunk of the table: bit j of word w: token w + 32 j has an entry (neighbours,
+                                     // the frequent tokens, fall to different lanes)
+  int32_t draft[ERSD_MAX_ROWS];
+  uint8_t parent[ERSD_MAX_ROWS];
+  // behind it, where they are needed (room that is not taken lets more blocks onto an SM):
+  //   uint32_t bias_at[kSpan];                              1 + index of the token's bias
+  //   uint32_t mask[kLogitWarps][kMaskRing][2][32];         the one or two words in which a lane's bits are
 };
+constexpr size_t kBiasBytes = sizeof(uint32_t) * kSpan, kMaskBytes = sizeof(uint32_t) * kLogitWarps * kMaskRing * 32;
 
-template <typename T>
-__global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const LogitParams p) {
-  extern __shared__ uint32_t shared[];
-  const int b = blockIdx.x, tid = threadIdx.x;
-  const int s0 = (int)blockIdx.y * p.slice;               // this block: groups whose last token is in [s0, s0 + slice)
-  const int base = s0 - kGroup, span = p.slice + kGroup;  // tokens base .. base + span
-  uint32_t* table = shared;                               // [span] counts and flags
-  uint16_t* list = (uint16_t*)(table + span);             // [span] tokens of the table that occur
-  uint32_t* bias_at = table + span + span / 2;            // [span] 1 + index of the token's bias, where biases are given
-  __shared__ int32_t draft[ERSD_MAX_ROWS];
-  __shared__ uint8_t parent[ERSD_MAX_ROWS];
-  __shared__ int listed;
+// kVary: rows of the input start at different distances from a 16-byte boundary (else what a warp's chunk is, is
+// worked out once and not for every row).
+template <typename T, bool kVary>
+__global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __grid_constant__ LogitParams p) {
+  extern __shared__ __align__(128) char raw[];
+  LogitShared<T>& sh = *(LogitShared<T>*)raw;
+  uint32_t* const bias_at = (uint32_t*)(raw + sizeof sh);
+  const bool own_biases = p.bias_count && p.long_history;
+  constexpr int kPer16 = 16 / (int)sizeof(T);
+  const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int s0 = (int)blockIdx.y * kSlice;
+  // Chunks start on 16-byte boundaries of the input, `lead` tokens before the slice's own start.  Where all rows
+  // have the same lead the table starts there, and a warp's chunk is a chunk of the table; else it starts kLead
+  // before, and a warp's chunk of a row lies in two chunks of the table.
+  auto lead_of = [&](int r) {
+    return (int)(((uintptr_t)((const T*)p.in + ((int64_t)b * p.R + r) * p.ld_in) / sizeof(T)) & (kPer16 - 1));
+  };
+  const int base = s0 - (kVary ? kLead : lead_of(0));
   const bool changes = p.history || p.draft_tokens || p.bias_count;
+  // (a lane's bits are one word where the rows' chunks start on words, as in rows on 16-byte boundaries)
+  const int per_row = kVary || lead_of(0) ? 64 : 32;
+  uint32_t* const masks = bias_at + (own_biases ? kSpan : 0) + warp * (kMaskRing * per_row) + lane;
   if (changes) {
-    for (int i = tid; i < span; i += kLogitThreads) table[i] = 0;
-    if (p.bias_count)
-      for (int i = tid; i < span; i += kLogitThreads) bias_at[i] = 0;
+    for (int i = tid; i < kSpan; i += kLogitThreads) sh.table[i] = 0;
+    if (own_biases)
+      for (int i = tid; i < kSpan; i += kLogitThreads) bias_at[i] = 0;
     if (p.tree)
-      for (int n = tid; n < ERSD_MAX_ROWS; n += kLogitThreads) parent[n] = p.parent[n];
-    if (tid == 0) listed = 0;
+      for (int n = tid; n < ERSD_MAX_ROWS; n += kLogitThreads) sh.parent[n] = p.parent[n];
+    if (tid < kLists * 32) sh.touched[tid >> 5][tid & 31] = 0;
   }
+  if (warp < kLogitWarps && lane < kRing) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sh.full[warp][lane])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  // ---- the copy
-  constexpr int kPer16 = 16 / (int)sizeof(T);
-  const int mask_last = (p.V - 1) >> 5, groups = p.slice / kGroup, shift = __ffs(groups) - 1;
-  if (!p.in_place || p.mask) {
-    const int64_t items = (int64_t)p.R * groups;
-    for (int64_t i0 = tid; i0 < items; i0 += kLogitThreads * kAhead) {
-      Group<T> x[kAhead];
-      uint32_t allow[kAhead];
-      int t[kAhead];
-      const T* in[kAhead];
-      // groups start on 16-byte boundaries of the input: `lead` tokens before the slice's first
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int64_t i = i0 + k * kLogitThreads;
-        const int r = (int)(i >> shift), g = (int)(i & (groups - 1));
-        in[k] = (const T*)p.in + ((int64_t)b * p.R + r) * p.ld_in;
-        t[k] = i < items ? s0 - (int)(((uintptr_t)in[k] / sizeof(T)) & (kPer16 - 1)) + g * kGroup : p.V;
-        allow[k] = 0xFFu;
-        if (p.mask && t[k] >= 0 && t[k] + kGroup <= p.V)
-          allow[k] = bits_at(p.mask + b * p.mask_stride_b + r * p.mask_stride_r, t[k], mask_last);
-      }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (t[k] >= 0 && t[k] + kGroup <= p.V && allow[k] && (!p.in_place || allow[k] != 0xFFu)) {
-#pragma unroll
-          for (int j = 0; j < Group<T>::kWords / 4; ++j) ((int4*)&x[k])[j] = __ldg((const int4*)(in[k] + t[k]) + j);
-        }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (t[k] >= p.V || t[k] + kGroup <= 0) continue;
-        const int r = (int)((i0 + k * kLogitThreads) >> shift);
-        T* out = (T*)p.out + ((int64_t)b * p.R + r) * p.ld_out;
-        if (t[k] < 0 || t[k] + kGroup > p.V) {  // cut by the row's ends
-          const uint32_t* mask = p.mask ? p.mask + b * p.mask_stride_b + r * p.mask_stride_r : nullptr;
-          for (int i = max(t[k], 0); i < min(t[k] + kGroup, p.V); ++i)
-            out[i] = !mask || (mask[i >> 5] >> (i & 31) & 1u) ? in[k][i] : from_float<T>(-INFINITY);
-          continue;
-        }
-        if (p.in_place && allow[k] == 0xFFu) continue;
-        x[k].forbid(allow[k]);
-        if (((uintptr_t)(out + t[k]) & 15) == 0) {
-#pragma unroll
-          for (int j = 0; j < Group<T>::kWords / 4; ++j) ((int4*)(out + t[k]))[j] = ((const int4*)&x[k])[j];
-        } else {
-#pragma unroll
-          for (int e = 0; e < kGroup; ++e) out[t[k] + e] = ((const T*)&x[k])[e];
-        }
-      }
-    }
-  }
-  if (!changes) return;
-  __syncthreads();  // (the table is zeros)
-
-  // ---- the tokens that are changed
-  auto put = [&](int t, uint32_t flags, uint32_t count) {
-    const int at = t - base;
-    if (t < 0 || t >= p.V || at < 0 || at >= span) return;
-    if (atomicOr(&table[at], flags) == 0) list[atomicAdd(&listed, 1)] = (uint16_t)at;
-    if (count) atomicAdd(&table[at], count);
+  const int mask_words = (p.V + 31) >> 5;
+  struct Piece {     // a warp's chunk of a row: tokens [lo, hi), of which [a, z) lie in whole 16 bytes
+    int start, lo, hi, a, z;
   };
-  if (p.history) {
-    int n = p.history_lens ? p.history_lens[b] : p.history_width;
-    n = max(0, min(n, p.history_width));
-    const int prompt = p.prompt_lens ? p.prompt_lens[b] : 0;
-    const int32_t* h = p.history + (int64_t)b * p.history_width;
-#pragma unroll 4
-    for (int i = tid; i < n; i += kLogitThreads) put(h[i], kSeen, i >= prompt);
-  }
-  const int drafts = p.draft_tokens ? p.R - 1 : 0;  // draft[n], 1 <= n <= drafts: token of node n
-  for (int n = 1 + tid; n <= drafts; n += kLogitThreads) {
-    const int t = p.tree ? p.draft_tokens[(int64_t)b * p.R + n] : p.draft_tokens[(int64_t)b * (p.R - 1) + n - 1];
-    draft[n] = t;
-    put(t, kDrafted, 0);
-  }
-  for (int i = tid; i < p.bias_count; i += kLogitThreads) {
-    const int t = p.bias_tokens[b * p.bias_stride + i], at = t - base;
-    if (t >= 0 && t < p.V && at >= 0 && at < span) atomicMax(&bias_at[at], (uint32_t)i + 1u);
-    put(t, kBiased, 0);
-  }
-  const float rep = p.repetition ? p.repetition[b] : 1.0f;
-  const float pres = p.presence ? p.presence[b] : 0.0f;
-  const float freq = p.frequency ? p.frequency[b] : 0.0f;
-  const float* bias = p.bias_count ? p.bias_values + b * p.bias_stride : nullptr;
-  __syncthreads();  // (the list; and the copies of other threads, which are written over)
-  const int n = listed;
-  const int items = n * p.R;  // (at most 4104 * 65535)
-  for (int i0 = tid; i0 < items; i0 += kLogitThreads * kAhead) {
-    float x[kAhead];
-    int r[kAhead], at[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int i = i0 + k * kLogitThreads;
-      at[k] = -1;
-      if (i >= items) continue;
-      r[k] = i / n;
-      const int found = list[i - r[k] * n], t = found + base;
-      const T* in = (const T*)p.in + ((int64_t)b * p.R + r[k]) * p.ld_in;
-      // the token's group may belong to the block before or behind this one in this row
-      const int lead = (int)(((uintptr_t)in / sizeof(T)) & (kPer16 - 1));
-      if (t < s0 - lead || t >= s0 - lead + p.slice) continue;
-      if (p.mask && !(p.mask[b * p.mask_stride_b + r[k] * p.mask_stride_r + (t >> 5)] >> (t & 31) & 1u)) continue;
-      at[k] = found;
-      x[k] = to_float(in[t]);
+  auto piece_of = [&](int r) {
+    Piece c;
+    c.start = s0 - lead_of(r) + warp * kChunk;
+    c.lo = max(c.start, 0);
+    c.hi = min(c.start + kChunk, p.V);
+    c.a = c.start + (c.lo - c.start + kPer16 - 1) / kPer16 * kPer16;
+    c.z = c.start + (max(c.hi, c.start) - c.start) / kPer16 * kPer16;
+    if (c.z < c.a) c.a = c.z = max(c.hi, c.lo);  // (none: the ends take all)
+    return c;
+  };
+  const Piece first = piece_of(0);
+  const T* const in0 = (const T*)p.in + (int64_t)b * p.R * p.ld_in;
+  T* const out0 = (T*)p.out + (int64_t)b * p.R * p.ld_out;
+  const uint32_t* const mask0 = p.mask ? p.mask + b * p.mask_stride_b : nullptr;
+  // This lane's 32 bits of row r's mask lie in one word or two, which are asked for kMaskRing - 1 rows ahead.
+  auto ask_mask = [&](int r) {
+    if (p.mask && r < p.R) {
+      const int bit = (kVary ? piece_of(r).start : first.start) + lane * 32, w = bit >> 5;
+      const uint32_t* m = mask0 + r * p.mask_stride_r;
+      const bool lo = w >= 0 && w < mask_words, hi = (bit & 31) && w + 1 >= 0 && w + 1 < mask_words;
+      copy_word(masks + r % kMaskRing * per_row, lo ? m + w : m, lo);
+      if (per_row == 64) copy_word(masks + r % kMaskRing * per_row + 32, hi ? m + w + 1 : m, hi);
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (at[k] < 0) continue;
-      const int t = at[k] + base;
-      const uint32_t e = table[at[k]];
-      uint32_t c = e & kCount;
-      bool seen = (e & kSeen) != 0;
-      if (e & kDrafted) {  // a drafted token counts if it is on the path to this row
-        for (int m = r[k]; m > 0; m = p.tree ? parent[m] : m - 1) c += draft[m] == t;
-        seen |= c > 0;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto bits_of = [&](int r) {
+    if (!p.mask) return 0xFFFFFFFFu;
+    if (per_row == 32) return masks[r % kMaskRing * per_row];
+    const int bit = (kVary ? piece_of(r).start : first.start) + lane * 32;
+    return __funnelshift_r(masks[r % kMaskRing * per_row], masks[r % kMaskRing * per_row + 32], bit & 31);
+  };
+  // Asks for the warp's chunk of row r, unless `allow` (this lane's bits) has nothing in any lane.
+  auto load = [&](int r, uint32_t allow) {
+    const Piece c = kVary ? piece_of(r) : first;
+    T* to = sh.ring[warp][r % kRing];
+    const T* in = in0 + r * p.ld_in;
+    const bool wanted = __any_sync(0xFFFFFFFFu, allow != 0) && c.lo < c.hi;
+    if (lane == 0) {
+      const uint32_t bytes = wanted ? (uint32_t)(c.z - c.a) * (uint32_t)sizeof(T) : 0u, full = shared_address(&sh.full[warp][r % kRing]);
+      if (bytes) {
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full), "r"(bytes) : "memory");
+        bulk_load(to + (c.a - c.start), in + c.a, bytes, &sh.full[warp][r % kRing]);
+      } else {
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full) : "memory");
       }
-      float y = x[k];
-      if (seen) {
-        if (p.repetition) y = y > 0.0f ? __fdiv_rn(y, rep) : y * rep;
-        if (c) y = y - freq * (float)c - pres;
-      }
-      if (e & kBiased) y += bias[bias_at[at[k]] - 1];
-      ((T*)p.out + ((int64_t)b * p.R + r[k]) * p.ld_out)[t] = from_float<T>(y);
     }
-  }
-}
+    if (wanted && (c.a > c.lo || c.z < c.hi)) {  // the row's ends, which no bulk copy takes
+      for (int t = c.lo + lane; t < min(c.a, c.hi); t += 32) to[t - c.start] = in[t];
+      for (int t = max(c.z, c.lo) + lane; t < c.hi; t += 32) to[t - c.start] = in[t];
+    }
+  };
 
-size_t logit_smem(int slice, bool biases) {
-  const size_t span = (size_t)slice + kGroup;
-  return 4 * (span + span / 2 + (biases ? span : 0));
+  const bool streams = (!p.in_place || p.mask) && warp < kLogitWarps;
+  if (streams) {
+#pragma unroll
+    for (int r = 0; r < kMaskRing - 1; ++r) ask_mask(r);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kMaskRing - kRing) : "memory");
+#pragma unroll
+    for (int r = 0; r < kRing - 1; ++r)
+      if (r < p.R) load(r, bits_of(r));
+  }
+
+  float rep = 1.0f, pres = 0.0f, freq = 0.0f;
+  const float* bias = nullptr;
+  if (changes) {
+    if (p.repetition) rep = p.repetition[b];
+    if (p.presence) pres = p.presence[b];
+    if (p.frequency) freq = p.frequency[b];
+    if (p.bias_count) bias = p.bias_values + b * p.bias_stride;
+    __syncthreads();  // (the table is zeros)
+    auto place_of = [&](int t) { return t >= 0 && t < p.V && t >= base && t - base < kSpan ? t - base : -1; };
+    auto touch = [&](int at) { atomicOr(&sh.touched[at / kChunk][at & 31], 1u << (at / 32 & 31)); };
+    for (int i = tid; i < p.bias_count; i += kLogitThreads) {
+      const int at = place_of(p.bias_tokens[b * p.bias_stride + i]);
+      if (at < 0) continue;
+      if (own_biases) {
+        atomicMax(&bias_at[at], (uint32_t)i + 1u);
+        atomicOr(&sh.table[at], kBiased);
+      } else {  // (the table holds nothing else yet: the largest is the last of the token's)
+        atomicMax(&sh.table[at], kBiased | ((uint32_t)i + 1u) << kBiasShift);
+      }
+      touch(at);
+    }
+    if (p.bias_count) __syncthreads();
+    const int drafts = p.draft_tokens ? p.R - 1 : 0;  // draft[n], 1 <= n <= drafts: token of node n
+    for (int n = 1 + tid; n <= drafts; n += kLogitThreads) {
+      const int t = p.tree ? p.draft_tokens[(int64_t)b * p.R + n] : p.draft_tokens[(int64_t)b * (p.R - 1) + n - 1];
+      sh.draft[n] = t;
+      const int at = place_of(t);
+      if (at < 0) continue;
+      atomicOr(&sh.table[at], kDrafted);
+      touch(at);
+    }
+    if (p.history) {
+      int n = p.history_lens ? p.history_lens[b] : p.history_width;
+      n = max(0, min(n, p.history_width));
+      const int prompt = p.prompt_lens ? p.prompt_lens[b] : 0;
+      const int32_t* h = p.history + (int64_t)b * p.history_width;
+      for (int i0 = tid; i0 < p.history_width && (i0 < 8 * kLogitThreads || i0 < n); i0 += 8 * kLogitThreads) {
+        int t[8];  // (asked for before the length is known to be so: the entries up to the width are there)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = i0 + k * kLogitThreads < p.history_width ? h[i0 + k * kLogitThreads] : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (i0 + k * kLogitThreads >= n) t[k] = -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = place_of(t[k]);
+          if (at < 0) continue;
+          atomicOr(&sh.table[at], kSeen);
+          if (i0 + k * kLogitThreads >= prompt) atomicAdd(&sh.table[at], 1u);
+          touch(at);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const uint32_t count_bits = p.long_history ? kLongCount : kShortCount;
+  // The logit x of the table's token `at` on row r.
+  auto changed = [&](float x, int at, int r) {
+    const uint32_t e = sh.table[at];
+    uint32_t c = e & count_bits;
+    bool seen = (e & kSeen) != 0;
+    if (e & kDrafted) {  // a drafted token counts if it is on the path to this row
+      for (int m = r; m > 0; m = p.tree ? sh.parent[m] : m - 1) c += sh.draft[m] == at + base;
+      seen |= c > 0;
+    }
+    if (seen) {
+      if (p.repetition) x = x > 0.0f ? __fdiv_rn(x, rep) : x * rep;
+      if (c) x -= fmaf(freq, (float)c, pres);
+    }
+    if (e & kBiased) x += bias[(p.long_history ? bias_at[at] : e >> kBiasShift & 0xFFFFu) - 1];
+    return x;
+  };
+
+  if (p.in_place && !p.mask) {  // the listed tokens alone
+    if (!changes) return;
+    for (int l = warp; l < kLists; l += 2 * kLogitWarps) {
+      for (int r = 0; r < p.R; ++r) {
+        const int lead = lead_of(r);
+        for (uint32_t left = sh.touched[l][lane]; left; left &= left - 1) {
+          const int at = l * kChunk + lane + 32 * (__ffs(left) - 1), t = at + base;
+          if (t < s0 - lead || t >= s0 - lead + kSlice) continue;  // (in this row the token is in another block's slice)
+          T* x = (T*)p.out + ((int64_t)b * p.R + r) * p.ld_out + t;
+          *x = from_float<T>(changed(to_float(*x), at, r));
+        }
+      }
+    }
+    return;
+  }
+
+  if (!streams) return;
+  const uint32_t my_touched = changes ? sh.touched[warp][lane] : 0u;
+  for (int r = 0; r < p.R; ++r) {
+    const Piece c = kVary ? piece_of(r) : first;
+    T* x = sh.ring[warp][r % kRing];
+    {
+      const uint32_t full = shared_address(&sh.full[warp][r % kRing]), parity = (uint32_t)(r / kRing) & 1;
+      uint32_t ok = 0;
+      for (int i = 0; i < (1 << 22) && !ok; ++i)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok)
+                     : "r"(full), "r"(parity)
+                     : "memory");
+      // (a copy that never lands: seen by whoever reads the row)
+      if (!__all_sync(0xFFFFFFFFu, ok)) {
+        for (int i = lane; i < kChunk; i += 32) x[i] = from_float<T>(__uint_as_float(0x7FC00000u));
+      }
+    }
+    __syncwarp();
+    // ---- the listed tokens
+    if (changes) {
+      for (int l = warp; l <= warp + (kVary ? 1 : 0); ++l) {
+        for (uint32_t left = kVary ? sh.touched[l][lane] : my_touched; left; left &= left - 1) {
+          const int at = l * kChunk + lane + 32 * (__ffs(left) - 1), in_chunk = at + base - c.start;
+          if (kVary && (in_chunk < 0 || in_chunk >= kChunk)) continue;
+          x[in_chunk] = from_float<T>(changed(to_float(x[in_chunk]), at, r));
+        }
+      }
+      __syncwarp();
+    }
+    const uint32_t bits = bits_of(r);
+    // ---- the mask: 32 tokens to a lane, which start at different ones of their 16-byte pieces (other banks)
+    if (p.mask && bits != 0xFFFFFFFFu) {
+      uint4* mine = (uint4*)(x + lane * 32);
+      constexpr int kPieces = 2 * (int)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const int k = (j + (lane >> (sizeof(T) == 2 ? 1 : 0))) & (kPieces - 1);
+        const uint32_t ok = bits >> (k * kPer16);
+        uint4 w = mine[k];
+        uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(T) == 4) {
+            v[i] = ok >> i & 1u ? v[i] : 0xFF800000u;
+          } else {
+            // (all bits of a half as its token's bit, which the shifts bring to the top)
+            const uint32_t keep = spread_tops(ok << (30 - 2 * i), ok << (31 - 2 * i));
+            v[i] = (v[i] & keep) | (0xFF80FF80u & ~keep);
+          }
+        }
+        mine[k] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    }
+    // ---- the next row to ask for takes the place of the one before this, which has been taken away meanwhile
+    ask_mask(r + kMaskRing - 1);
+    if (r + kRing - 1 < p.R) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kMaskRing - kRing) : "memory");
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      __syncwarp();
+      load(r + kRing - 1, bits_of(r + kRing - 1));
+    }
+    T* out = out0 + r * p.ld_out;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (((uintptr_t)(out + c.a) & 15) == 0) {
+      if (lane == 0) {
+        if (c.z > c.a) bulk_store(out + c.a, x + (c.a - c.start), (uint32_t)(c.z - c.a) * (uint32_t)sizeof(T));
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+      if (c.a > c.lo || c.z < c.hi) {
+        for (int t = c.lo + lane; t < min(c.a, c.hi); t += 32) out[t] = x[t - c.start];
+        for (int t = max(c.z, c.lo) + lane; t < c.hi; t += 32) out[t] = x[t - c.start];
+      }
+    } else {  // rows of logits and out at different distances from a 16-byte boundary
+      for (int t = c.lo + lane; t < c.hi; t += 32) out[t] = x[t - c.start];
+    }
+    __syncwarp();
+  }
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // (shared memory goes with the block)
 }
 
 }  // namespace
@@ -254,7 +393,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
                          o.bias_values, o.mask};
   for (const void* w : words)
     if (!aligned_to(w, 4)) return ERSD_EALIGN;
-  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
+  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || o.history_width > (1 << 30) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
   if (o.draft_tokens && o.parent && !is_tree(o.parent, R)) return ERSD_EINVAL;
   LogitParams p;
   memset(&p, 0, sizeof p);
@@ -285,18 +424,18 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
   p.mask = o.mask;
   p.mask_stride_b = o.mask_stride_b;
   p.mask_stride_r = o.mask_stride_r;
-  // Long slices while there are four blocks to an SM (every block reads the sequence's whole history), shorter ones
-  // for few sequences.
-  p.slice = 4096;
-  while (p.slice > 1024 && (int64_t)B * ((V + p.slice - 1) / p.slice) < 4 * sm_count()) p.slice /= 2;
-  const unsigned slices = (unsigned)(((int64_t)V + kGroup - 1 + p.slice - 1) / p.slice);
-  const size_t smem = logit_smem(p.slice, p.bias_count != 0);
-  const auto kernel = dt == ERSD_BF16 ? process_logits_kernel<__nv_bfloat16> : process_logits_kernel<float>;
+  const unsigned slices = (unsigned)(((int64_t)V + kLead - 1 + kSlice - 1) / kSlice);
+  const bool vary = (int64_t)B * R > 1 && (p.ld_in * (int64_t)size & 15) != 0;
+  size_t smem = dt == ERSD_BF16 ? sizeof(LogitShared<__nv_bfloat16>) : sizeof(LogitShared<float>);
+  p.long_history = o.history && o.history_width > (int)kShortCount;
+  const bool lead = vary || !aligned_to(logits, 16);
+  smem += (p.bias_count && p.long_history ? kBiasBytes : 0) + (p.mask ? (lead ? 2 : 1) * kMaskBytes : 0);
+  const auto kernel = dt == ERSD_BF16 ? (vary ? process_logits_kernel<__nv_bfloat16, true> : process_logits_kernel<__nv_bfloat16, false>)
+                                      : (vary ? process_logits_kernel<float, true> : process_logits_kernel<float, false>);
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return cuda_fail(e);
-  note_launch("process_logits_kernel<%s>: %d threads x (%d, %u) blocks, slices of %d tokens", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads,
-              B, slices, p.slice);
+  note_launch("process_logits_kernel<%s>: %d threads x (%d, %u) blocks", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads, B, slices);
   // (all sequences' first slices before the next: frequent tokens have low numbers, their blocks the most to change)
   Launch l(dim3((unsigned)B, slices, 1), kLogitThreads, smem, (cudaStream_t)cuda_stream);
   e = cudaLaunchKernelEx(&l.cfg, kernel, p);
