@@ -1,12 +1,15 @@
 // ersd_chunk_attention on tensor cores: bfloat16 caches with heads of 64 or 128.
 //
-// A thread block takes 128 or 256 packed rows of one kv head (see AttentionParams) through its keys, 128 slots at
-// a time.  One warp copies keys and values page by page with TMA into a ring of shared memory, one thread issues
-// the products (tcgen05.mma), and two groups of four warps do the softmax, a thread to a row: scores come out of
-// tensor memory, weights go back there as bfloat16 over the scores they came from, and the second product takes
-// them from there.  The two groups work on two independent streams, so that one's products run while the other's
-// softmax does: with 256 rows a stream is half of the rows; with up to 128, where the cache's bytes bound the
-// call, both streams have the same rows and take turns at the tiles of keys, and are joined at the end.
+// A thread block takes a tile of packed rows of one kv head (see AttentionParams) through its keys.  One warp
+// copies keys and values page by page with TMA into a ring of shared memory, one thread issues the products
+// (tcgen05.mma), and groups of four warps do the softmax, a thread to a row: scores come out of tensor memory,
+// weights go back there as bfloat16 over scores they came from, and the second product takes them from there.
+// Two builds:
+//   Few<D>   up to 128 packed rows (decoding, drafts), where the cache's bytes bound the call: 64 slots at a time,
+//            scores in two buffers so that the next product of scores runs during a softmax, half of an SM's shared
+//            and tensor memory, so that two blocks share an SM and one's start and end hide behind the other.
+//   Many<D>  256 packed rows (long chunks), where products and powers of two do: two streams of 128 rows with a
+//            softmax group each, 128 slots at a time; one's products run while the other's softmax does.
 //
 // The output's accumulator stays in tensor memory.  It is scaled only when a row's maximum has risen by more than
 // 2^8 since the last time (weights are then at most 2^8, which bfloat16 and the 32-bit sums hold as well as 1);
@@ -28,35 +31,53 @@ namespace ersd {
 
 namespace {
 
-constexpr int kN = 128;               // slots of a tile of keys
-constexpr int kSoftmaxThreads = 256;  // two groups of four warps
-constexpr int kTensorThreads = kSoftmaxThreads + 64;
 constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before its output is scaled
 
-template <int D, int NT>
-struct Plan {
-  static constexpr int kStageBytes = kN * D * 2;                                   // keys or values of a tile
-  static constexpr int kStages = D == 64 ? 12 : NT == 1 ? 6 : 5;
-  static constexpr int kQBytes = NT * 128 * D * 2;
-  static constexpr int kRows = NT * 128;
-  // (the largest is all that a block may have; every one is more than half of it, so that no two blocks, each
-  // with all of the tensor memory, ever meet on an SM)
-  static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes + 1024;
-  static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
-  static_assert(kRows * (kPartRow + 2) * 4 <= kStages * kStageBytes, "");
-  static_assert(kSmem <= 232448 && kSmem > 120000, "");
+template <int D_>
+struct Few {
+  static constexpr int D = D_, kStreams = 1, kN = 64, kBuffers = 2, kStages = D == 64 ? 8 : 4;
+  static constexpr int kWarps = 4, kThreads = 192, kBlocks = 2, kColumns = 256;
 };
+template <int D_>
+struct Many {
+  static constexpr int D = D_, kStreams = 2, kN = 128, kBuffers = 1, kStages = D == 64 ? 12 : 5;
+  // (two warps without work make the last four a group that gives its registers to the others)
+  static constexpr int kWarps = 8, kThreads = 384, kBlocks = 1, kColumns = 512;
+  static constexpr int kRegistersSoftmax = 216, kRegistersOthers = 72;  // 2 * 216 + 72 = 3 * 168, what a launch gives
+};
+
+constexpr int kTableRing = 8;  // tiles whose table entries are on their way or in use
 
 struct Misc {  // behind the ring
   uint64_t full[12], empty[12];  // of the ring's stages
-  uint64_t scores[2];            // a stream's scores are in tensor memory
-  uint64_t weights[2];           // and its weights, instead of them
+  uint64_t scores[2];            // of a stream (or a buffer) are in tensor memory
+  uint64_t weights[2];           // and the weights that take their place.  (A buffer's own: with one barrier for both
+                                 // a quick warp's next tile would count for a slow warp's last.)
+  uint64_t rest[2];              // a stream's output is at rest: the product with the last weights is done
   uint64_t done;                 // all products
   uint32_t tmem;
   uint32_t gave_up;              // a wait ran out: nothing that follows it can be trusted
+  int32_t entries[kTableRing][32];
   uint8_t parent[ERSD_MAX_ROWS], depth[ERSD_MAX_ROWS];
 };
-static_assert(sizeof(Misc) <= 1024, "");
+static_assert(sizeof(Misc) <= 2048, "");
+
+template <typename C>
+struct Plan : C {
+  static constexpr int D = C::D, kN = C::kN, kStages = C::kStages;
+  static constexpr int kRows = C::kStreams * 128;
+  static constexpr int kStageBytes = kN * D * 2;  // keys or values of a tile
+  static constexpr int kQBytes = kRows * D * 2;
+  static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes + 2048;
+  static constexpr int kOutputs = C::kStreams * C::kBuffers * kN;  // first column of the outputs
+  static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
+  static_assert(kRows * (kPartRow + 2) * 4 <= kQBytes + kStages * kStageBytes, "");
+  static_assert(kOutputs + C::kStreams * D <= C::kColumns, "");
+  // No more than kBlocks blocks fit on an SM by shared memory, and their tensor memory fits with them: a block
+  // never waits for another's tensor memory, which could not be given up by one that waits for it in a cluster.
+  static_assert((kSmem + 1024) * C::kBlocks <= 228 * 1024 && (kSmem + 1024) * (C::kBlocks + 1) > 228 * 1024, "");
+  static_assert(C::kBlocks * C::kColumns <= 512, "");
+};
 
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -159,6 +180,32 @@ __device__ __forceinline__ uint32_t pair(float lo, float hi) {
   return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// Two 32-bit floats in a register pair, and what is done to both at once.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void apart(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ void copy_entry(int32_t* to, const int32_t* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_address(to)), "l"(from) : "memory");
+}
+
 // Bits [a, b) of a word, both cut to 0..32.
 __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   a = max(a, 0);
@@ -167,46 +214,37 @@ __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   return (0xFFFFFFFFu >> (32 - (b - a))) << a;
 }
 
-// The order in which the ring is filled is the order of use.  Step u of the products is tile tile_of(u) for stream
-// u & 1; with 256 rows both streams use every tile (NT = 2: steps 2t and 2t + 1), else a tile has one step.
-// Items: the keys of the first tiles, then by step its values and the keys of that stream's next tile.
-template <int NT>
+// The order in which the ring is filled is the order of use: the keys of the first kBuffers tiles, then by tile its
+// values and the keys of the tile kBuffers on.
+template <int kBuffers>
 struct Order {
   int tiles;
   __device__ __forceinline__ int items() const { return 2 * tiles; }
-  __device__ __forceinline__ int keys_of(int t) const {
-    if (NT == 2) return 2 * t;
-    return t < 2 ? t : min(tiles, 2) + 2 * (t - 2) + 1;
-  }
-  __device__ __forceinline__ int values_of(int t) const {
-    if (NT == 2) return 2 * t + 1;
-    return min(tiles, 2) + t + min(t, max(tiles - 2, 0));
-  }
+  __device__ __forceinline__ int keys_of(int t) const { return t < kBuffers ? t : min(tiles, kBuffers) + 2 * (t - kBuffers) + 1; }
+  __device__ __forceinline__ int values_of(int t) const { return min(tiles, kBuffers) + t + min(t, max(tiles - kBuffers, 0)); }
   // item q: its tile; whether it is values
   __device__ __forceinline__ int tile(int q, bool* values) const {
-    if (NT == 2) {
-      *values = q & 1;
-      return q >> 1;
-    }
-    const int first = min(tiles, 2);
+    const int first = min(tiles, kBuffers);
     *values = false;
     if (q < first) return q;
-    const int x = q - first, both = 2 * max(tiles - 2, 0);  // values 0, keys 2, values 1, keys 3, ...
+    const int x = q - first, both = 2 * max(tiles - kBuffers, 0);
     if (x < both) {
       *values = !(x & 1);
-      return (x >> 1) + (x & 1) * 2;
+      return (x >> 1) + (x & 1) * kBuffers;
     }
     *values = true;
     return (both >> 1) + x - both;
   }
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(kTensorThreads, 1)
+template <typename C>
+__global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     attention_tensor_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map,
                             const __grid_constant__ CUtensorMap v_map, const int box) {
-  using P = Plan<D, NT>;
-  constexpr int kStages = P::kStages, kPanel = kN * 128;  // bytes of a panel: 128 rows of 64 elements
+  using P = Plan<C>;
+  constexpr int D = P::D, kN = P::kN, kStages = P::kStages, kStreams = C::kStreams, kBuffers = C::kBuffers;
+  constexpr int kPanel = kN * 128, kQPanel = 128 * 128;  // bytes of a panel: rows of 64 elements
+  constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = C::kWarps + 1;  // (the last two: warps)
   extern __shared__ char raw[];
   char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   char* q_tile = base;
@@ -218,13 +256,13 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int rows = p.row_counts ? p.row_counts[b] : p.R;
+  const int ctx = max(0, p.context_lens[b]);
   rows = max(0, min(rows, p.R));
   const int m0 = tile * P::kRows, m1 = min(m0 + P::kRows, rows * p.group);
   if (m0 >= m1) return;  // (the same for every block of the cluster)
-  const int ctx = max(0, p.context_lens[b]);
   const int r0 = m0 / p.group, r1 = (m1 - 1) / p.group + 1;
   // warps of each stream with rows
-  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = NT == 1 ? warps0 : (max(m1 - m0 - 128, 0) + 31) / 32;
+  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
   int min_depth = r0;
   if (p.tree) {
     min_depth = p.depth[r0];
@@ -232,7 +270,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
   }
   const KeyRange keys = key_range<kN>(p, ctx, r1, min_depth);
   const int t0 = (int)((int64_t)keys.tiles * part / p.split), t1 = (int)((int64_t)keys.tiles * (part + 1) / p.split);
-  const Order<NT> order{t1 - t0};
+  const Order<kBuffers> order{t1 - t0};
   const int tiles = t1 - t0;
 
   if (tid == 0) {
@@ -242,18 +280,19 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
     }
     for (int s = 0; s < 2; ++s) {
       barrier_init(&sh.scores[s], 1);
-      barrier_init(&sh.weights[s], (uint32_t)max(1, s ? warps1 : warps0));
+      barrier_init(&sh.weights[s], (uint32_t)max(1, s && kStreams == 2 ? warps1 : warps0));
+      barrier_init(&sh.rest[s], 1);
     }
     barrier_init(&sh.done, 1);
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_address(&sh.tmem)) : "memory");
+  if (warp == kProducts) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&sh.tmem)), "n"(C::kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (p.tree)
-    for (int n = tid; n < ERSD_MAX_ROWS; n += kTensorThreads) {
+    for (int n = tid; n < ERSD_MAX_ROWS; n += C::kThreads) {
       sh.parent[n] = p.parent[n];
       sh.depth[n] = p.depth[n];
     }
@@ -278,7 +317,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
       x.z ^= flip;
       x.w ^= flip;
       const int row = m & 127;
-      *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
+      *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kQPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -288,103 +327,116 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
   const uint32_t tmem = sh.tmem;
   uint32_t* const gave_up = &sh.gave_up;
 
-  float top = -INFINITY, sum = 0.f;  // of the row of a softmax thread: the maximum its weights were formed with, their sum
-  if (warp == 8) {
-    // ---- copies: a lane has one box (`box` slots by 64 elements) of every item
-    const int boxes = kN / box, group = lane % boxes, panel = lane / boxes;
-    const bool mine = panel < D / 64;
-    const int32_t* table = p.table + b * p.table_stride;
-    auto entry = [&](int q, bool* needed) {  // page of this lane's box of item q
-      bool values;
-      *needed = false;
-      if (!mine || q >= order.items()) return 0;
-      const int slot = tile_start<kN>(keys, t0 + order.tile(q, &values)) + group * box;
-      *needed = slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo);
-      return *needed ? table[slot / p.page_size] : 0;
-    };
-    constexpr int kAhead = 4;  // items whose table entries are asked for early
-    int page[kAhead];
-    bool needed[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) page[j] = entry(j, &needed[j]);
-    int q = 0;
-    for (; q < order.items(); ++q) {
-      const int stage = q % kStages;
-      const int page_now = page[0];
-      const bool needed_now = needed[0];
-#pragma unroll
-      for (int j = 0; j + 1 < kAhead; ++j) {
-        page[j] = page[j + 1];
-        needed[j] = needed[j + 1];
+  float* parts = (float*)base;                         // [rows][kPartRow]
+  float* tops = parts + P::kRows * P::kPartRow;        // [rows]
+  float* sums = tops + P::kRows;                       // [rows]
+  auto products_done = [&]() {
+    // (asked for in every case: after a wait that ran out, products may still be under way)
+    if (tiles > 0)
+      for (int i = 0; i < (1 << 22) && !barrier_try(&sh.done, 0); ++i) {
       }
-      page[kAhead - 1] = entry(q + kAhead, &needed[kAhead - 1]);
-      if (q >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], (uint32_t)(q / kStages - 1) & 1, gave_up))) break;
-      bool values;
-      const int slot = tile_start<kN>(keys, t0 + order.tile(q, &values)) + group * box;
-      const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, needed_now));
-      if (lane == 0) barrier_expect(&sh.full[stage], count * (uint32_t)box * 128u);
-      __syncwarp();
-      // (page numbers outside the cache give zeros)
-      if (needed_now)
-        tma_box(smem_address(ring + stage * P::kStageBytes + panel * kPanel + group * box * 128), values ? &v_map : &k_map, panel * 64,
-                slot % p.page_size, kv_head, page_now < 0 || page_now >= p.num_pages ? p.num_pages : page_now, &sh.full[stage]);
-      __syncwarp();
-    }
-    // every copy has landed before the block ends, even where the products gave up
-    if (*(volatile uint32_t*)gave_up)
-      for (int x = max(0, q - kStages); x < q; ++x)
-        for (int i = 0; i < (1 << 22) && !barrier_try(&sh.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
-        }
-  } else if (warp == 9) {
-    // ---- products
-    if (lane == 0 && tiles > 0) {
-      constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
-      const int steps = NT == 2 ? 2 * tiles : tiles;
-      const bool second = NT == 2 ? warps1 > 0 : tiles > 1;  // whether stream 1 has anything
-      bool ok = true;
-      auto wait_item = [&](int q) { return barrier_wait(&sh.full[q % kStages], (uint32_t)(q / kStages) & 1, gave_up); };
-      auto score = [&](int s, int t) {  // scores of stream s with tile t
-        const int item = order.keys_of(t);
-        if (!wait_item(item)) return false;
-        after_sync();
-        const uint32_t a = smem_address(q_tile) + (NT == 2 ? s * 128 * D * 2 : 0), k = smem_address(ring + (item % kStages) * P::kStageBytes);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          const uint32_t at = (j >> 2) * kPanel + (j & 3) * 32;
-          mma_shared(tmem + s * kN, operand(a + at, 16), operand(k + at, 16), kScores, j > 0);
-        }
-        mma_commit(&sh.scores[s]);
-        if (NT == 1 || s == 1 || !second) mma_commit(&sh.empty[item % kStages]);
-        return true;
-      };
-      ok = score(0, 0);
-      if (ok && second) ok = score(1, NT == 2 ? 0 : 1);
-      for (int u = 0; ok && u < steps; ++u) {
-        const int s = u & 1, i = u >> 1, t = NT == 2 ? i : u;
-        if (s == 1 && !second) continue;
-        if (!barrier_wait(&sh.weights[s], (uint32_t)i & 1, gave_up)) break;
-        const int item = order.values_of(t);
-        if (!wait_item(item)) break;
-        after_sync();
-        const uint32_t v = smem_address(ring + (item % kStages) * P::kStageBytes);
-#pragma unroll
-        for (int j = 0; j < kN / 16; ++j)
-          mma_tmem(tmem + 2 * kN + s * D, tmem + s * kN + j * 8, operand(v + j * 16 * 128, kPanel), kOutput, i > 0 || j > 0);
-        if (NT == 1 || s == 1 || !second) mma_commit(&sh.empty[item % kStages]);
-        const int next = NT == 2 ? t + 1 : t + 2;
-        if (next < tiles) ok = score(s, next);
-      }
-      mma_commit(&sh.done);
-    }
     __syncwarp();
+    after_sync();
+  };
+  if (warp >= C::kWarps) {
+    if constexpr (kStreams == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersOthers));
+    if (warp == kCopies) {
+      // ---- copies: a lane has one box (`box` slots by 64 elements) of every item.  Its entries of the block table
+      // come through shared memory, so that no register waits for them.
+      const int boxes = kN / box, group = lane % boxes, panel = lane / boxes;
+      const bool mine = panel < D / 64;
+      const int32_t* table = p.table + b * p.table_stride;
+      auto slot_of = [&](int t) { return tile_start<kN>(keys, t0 + t) + group * box; };
+      auto needs = [&](int slot) { return mine && slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo); };
+      auto ask = [&](int t) {
+        if (t < tiles) {
+          const int slot = slot_of(t);
+          if (needs(slot)) copy_entry(&sh.entries[t % kTableRing][lane], table + slot / p.page_size);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+      constexpr int kAhead = kTableRing - kBuffers - 1;  // (a tile's values come kBuffers tiles after its keys)
+#pragma unroll
+      for (int t = 0; t < kAhead; ++t) ask(t);
+      int q = 0;
+      for (; q < order.items(); ++q) {
+        const int stage = q % kStages;
+        bool values;
+        const int t = order.tile(q, &values), slot = slot_of(t);
+        const bool needed = needs(slot);
+        if (!values) {
+          ask(t + kAhead);
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        }
+        const int page = needed ? sh.entries[t % kTableRing][lane] : 0;
+        if (q >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], (uint32_t)(q / kStages - 1) & 1, gave_up))) break;
+        const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, needed));
+        if (lane == 0) barrier_expect(&sh.full[stage], count * (uint32_t)box * 128u);
+        __syncwarp();
+        // (page numbers outside the cache give zeros)
+        if (needed)
+          tma_box(smem_address(ring + stage * P::kStageBytes + panel * kPanel + group * box * 128), values ? &v_map : &k_map, panel * 64,
+                  slot % p.page_size, kv_head, page < 0 || page >= p.num_pages ? p.num_pages : page, &sh.full[stage]);
+        __syncwarp();
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      // every copy has landed before the block ends, even where the products gave up
+      if (*(volatile uint32_t*)gave_up)
+        for (int x = max(0, q - kStages); x < q; ++x)
+          for (int i = 0; i < (1 << 22) && !barrier_try(&sh.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
+          }
+      __syncwarp();
+    } else if (warp == kProducts) {
+      // ---- products
+      if (lane == 0 && tiles > 0) {
+        constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
+        const int streams = kStreams == 2 && warps1 > 0 ? 2 : 1;
+        bool ok = true;
+        auto wait_item = [&](int q) { return barrier_wait(&sh.full[q % kStages], (uint32_t)(q / kStages) & 1, gave_up); };
+        auto score = [&](int s, int t) {  // scores of stream s with tile t
+          const int item = order.keys_of(t), buffer = kBuffers == 2 ? t & 1 : s;
+          if (!wait_item(item)) return false;
+          after_sync();
+          const uint32_t a = smem_address(q_tile) + s * 128 * D * 2, k = smem_address(ring + (item % kStages) * P::kStageBytes);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+            mma_shared(tmem + buffer * kN, operand(a + (j >> 2) * kQPanel + (j & 3) * 32, 16), operand(k + (j >> 2) * kPanel + (j & 3) * 32, 16),
+                       kScores, j > 0);
+          mma_commit(&sh.scores[buffer]);
+          if (s == streams - 1) mma_commit(&sh.empty[item % kStages]);
+          return true;
+        };
+        for (int t = 0; ok && t < kBuffers && t < tiles; ++t)
+          for (int s = 0; ok && s < streams; ++s) ok = score(s, t);
+        for (int t = 0; ok && t < tiles; ++t)
+          for (int s = 0; ok && s < streams; ++s) {
+            const int item = order.values_of(t), buffer = kBuffers == 2 ? t & 1 : s;
+            ok = barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up);
+            if (!ok) break;
+            ok = wait_item(item);
+            if (!ok) break;
+            after_sync();
+            const uint32_t v = smem_address(ring + (item % kStages) * P::kStageBytes);
+#pragma unroll
+            for (int j = 0; j < kN / 16; ++j)
+              mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, operand(v + j * 16 * 128, kPanel), kOutput, t > 0 || j > 0);
+            if (kBuffers == 2) mma_commit(&sh.rest[s]);
+            if (s == streams - 1) mma_commit(&sh.empty[item % kStages]);
+            if (t + kBuffers < tiles) ok = score(s, t + kBuffers);
+          }
+        mma_commit(&sh.done);
+      }
+      __syncwarp();
+    }
+    products_done();
   } else {
     // ---- softmax: a thread has one row
+    if constexpr (kStreams == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersSoftmax));
     const int s = warp >> 2, quarter = warp & 3;
-    const int row = quarter * 32 + lane, m = m0 + (NT == 2 ? s * 128 : 0) + row;
+    const int row = quarter * 32 + lane, m = m0 + s * 128 + row;
     const int my_warps = s ? warps1 : warps0;
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t scores = tmem + lanes + s * kN, output = tmem + lanes + 2 * kN + s * D;
-    const int mine = NT == 2 ? tiles : s ? tiles / 2 : (tiles + 1) / 2;
+    float top = -INFINITY, sum = 0.f;  // the maximum that the row's weights were formed with, their sum
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, output = tmem + lanes + P::kOutputs + s * D;
     if (quarter < my_warps) {
       const float scale = fabsf(p.scale_log2);
       const int r = min(m, m1 - 1) / p.group;  // (rows of a warp behind the last: as the last, and not written)
@@ -393,13 +445,13 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
       const int hi = min(keys.hi, p.tree ? ctx : ctx + r + 1);
       const int sinks = p.window ? min(p.sinks, hi) : 0;
       // what the first and the last row of the stream see of the cache bounds the tiles that need no mask
-      const int first_m = m0 + (NT == 2 ? s * 128 : 0), last_m = min(first_m + 128, m1) - 1;
+      const int first_m = m0 + s * 128, last_m = min(first_m + 128, m1) - 1;
       const int all_hi = min(keys.hi, p.tree ? ctx : ctx + first_m / p.group + 1);
       const int all_lo = p.window ? ctx + (p.tree ? p.R - 1 : last_m / p.group) - p.window + 1 : 0;
-      for (int i = 0; i < mine; ++i) {
-        const int t = NT == 2 ? i : 2 * i + s;
-        const int start = tile_start<kN>(keys, t0 + t);
-        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.scores[s], (uint32_t)i & 1, gave_up))) break;
+      for (int t = 0; t < tiles; ++t) {
+        const int start = tile_start<kN>(keys, t0 + t), buffer = kBuffers == 2 ? t & 1 : s;
+        const uint32_t scores = tmem + lanes + buffer * kN;
+        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.scores[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up))) break;
         after_sync();
         uint32_t x[kN];
 #pragma unroll
@@ -407,9 +459,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
         tmem_loaded();
         const bool whole = start + kN <= all_hi && (start >= all_lo || start + kN <= p.sinks);
         if (!whole) {
-          uint32_t see[4];
+          uint32_t see[kN / 32];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
+          for (int w = 0; w < kN / 32; ++w) {
             const int at = start + 32 * w;
             see[w] = bits_between(lo - at, hi - at) | bits_between(-at, sinks - at);
           }
@@ -419,7 +471,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
               if (at >= 0 && at < kN && ctx + n < keys.hi && (!p.window || pos >= lo || pos < p.sinks)) {
                 const uint32_t bit = 1u << (at & 31);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) see[w] |= (at >> 5) == w ? bit : 0u;
+                for (int w = 0; w < kN / 32; ++w) see[w] |= (at >> 5) == w ? bit : 0u;
               }
               if (n == 0) break;
             }
@@ -449,15 +501,20 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
         }
         float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < kN; c += 4)
+        for (int c = 0; c < kN; c += 8)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) a[j] = fmaxf(a[j], __uint_as_float(x[c + j]));
-        const float now = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * scale;
+          for (int j = 0; j < 4; ++j) a[j] = max3(a[j], __uint_as_float(x[c + 2 * j]), __uint_as_float(x[c + 2 * j + 1]));
+        const float now = max3(fmaxf(a[0], a[1]), a[2], a[3]) * scale;
         const bool rise = now > top + kRise;  // (also from nothing seen to something)
-        if (i == 0) {
+        if (t == 0) {
           top = now;
         } else if (__any_sync(0xFFFFFFFFu, rise)) {
-          // (the scores of this tile come after the product with the last weights: the output is at rest)
+          // The output has to be at rest.  (With one buffer it is: this tile's scores come after the product with the
+          // last weights.)
+          if (kBuffers == 2) {
+            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.rest[s], (uint32_t)(t - 1) & 1, gave_up))) break;
+            after_sync();
+          }
           const float f = rise ? power_of_two(top - now) : 1.0f;
           sum *= f;
           if (rise) top = now;
@@ -472,120 +529,80 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
           }
         }
         const float minus = top == -INFINITY ? 0.f : -top;
-        float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale_two = two(scale, scale), minus_two = two(minus, minus);
+        uint64_t both[2] = {0, 0};
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < kN / 64; ++half) {
           uint32_t w[32];
 #pragma unroll
           for (int c = 0; c < 64; c += 2) {
-            const float e0 = power_of_two(fmaf(__uint_as_float(x[half * 64 + c]), scale, minus));
-            const float e1 = power_of_two(fmaf(__uint_as_float(x[half * 64 + c + 1]), scale, minus));
-            part_sum[c & 2] += e0;
-            part_sum[(c & 2) + 1] += e1;
+            float e0, e1;
+            apart(fma_two(two(__uint_as_float(x[half * 64 + c]), __uint_as_float(x[half * 64 + c + 1])), scale_two, minus_two), e0, e1);
+            e0 = power_of_two(e0);
+            e1 = power_of_two(e1);
+            both[c >> 1 & 1] = add_two(both[c >> 1 & 1], two(e0, e1));
             w[c >> 1] = pair(e0, e1);
           }
           tmem_store(scores + half * 32, w);
         }
-        sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+        float s0, s1;
+        apart(add_two(both[0], both[1]), s0, s1);
+        sum += s0 + s1;
         tmem_stored();
         before_sync();
         __syncwarp();
-        if (lane == 0) barrier_arrive(&sh.weights[s]);
+        if (lane == 0) barrier_arrive(&sh.weights[buffer]);
       }
     }
-  }
-
-  // ---- the end: every product is done, the ring is free
-  if (tiles > 0) {
-    // (asked for in every case: after a wait that ran out, products may still be under way)
-    for (int i = 0; i < (1 << 22) && !barrier_try(&sh.done, 0); ++i) {
-    }
-    __syncwarp();
-    after_sync();
-  }
-  if (warp < 8) {
-    const int s = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t output = tmem + ((uint32_t)(quarter * 32) << 16) + 2 * kN + s * D;
-    const int mine = NT == 2 ? tiles : s ? tiles / 2 : (tiles + 1) / 2;
-    const bool there = quarter < (s ? warps1 : warps0);
-    float* parts = (float*)ring;                         // [rows][kPartRow]
-    float* tops = parts + P::kRows * P::kPartRow;        // [rows]
-    float* sums = tops + P::kRows;                       // [rows]
-    const int m = m0 + (NT == 2 ? s * 128 : 0) + row;
-    float o[D];
-    if (there && mine > 0) {
-#pragma unroll
-      for (int c = 0; c < D; c += 32) tmem_load(output + c, (uint32_t*)o + c);
-      tmem_loaded();
-    } else {
-#pragma unroll
-      for (int c = 0; c < D; ++c) o[c] = 0.f;
-      top = -INFINITY;
-      sum = 0.f;
-    }
-    if (*(volatile uint32_t*)gave_up) sum = __uint_as_float(0x7FC00000u);  // NaN: seen by whoever reads the output
-    auto keep = [&]() {
-      const int at = NT == 2 ? s * 128 + row : row;
-#pragma unroll
-      for (int c = 0; c < D; c += 4) *(float4*)(parts + at * P::kPartRow + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-      tops[at] = top;
-      sums[at] = sum;
-    };
-    if (NT == 1) {
-      if (s == 1 && there) keep();
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (s == 0 && there && sums[row] != 0.f) {
-        const float other = tops[row], now = fmaxf(top, other), at = now == -INFINITY ? 0.f : now;
-        const float f = power_of_two(top - at), g = power_of_two(other - at);
-#pragma unroll
-        for (int c = 0; c < D; c += 4) {
-          const float4 x = *(const float4*)(parts + row * P::kPartRow + c);
-          o[c] = o[c] * f + x.x * g;
-          o[c + 1] = o[c + 1] * f + x.y * g;
-          o[c + 2] = o[c + 2] * f + x.z * g;
-          o[c + 3] = o[c + 3] * f + x.w * g;
-        }
-        sum = sum * f + sums[row] * g;
-        top = now;
-      }
-    }
-    const bool holds = there && (NT == 2 || s == 0);
+    // ---- the end: every product is done, q's rows and the ring are free
+    products_done();
     const bool wide = ((p.o_b | p.o_r | p.o_h) & 7) == 0 && ((uintptr_t)p.out & 15) == 0;
-    __nv_bfloat16* out = (__nv_bfloat16*)p.out + b * p.o_b;
-    if (p.split == 1) {
-      if (holds && m < m1) {
+    if (quarter < my_warps) {
+      float o[D];
+      if (tiles > 0) {
+#pragma unroll
+        for (int c = 0; c < D; c += 32) tmem_load(output + c, (uint32_t*)o + c);
+        tmem_loaded();
+      } else {
+#pragma unroll
+        for (int c = 0; c < D; ++c) o[c] = 0.f;
+      }
+      if (*(volatile uint32_t*)gave_up) sum = __uint_as_float(0x7FC00000u);  // NaN: seen by whoever reads the output
+      if (p.split > 1) {
+        const int at = s * 128 + row;
+#pragma unroll
+        for (int c = 0; c < D; c += 4) *(float4*)(parts + at * P::kPartRow + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+        tops[at] = top;
+        sums[at] = sum;
+      } else if (m < m1) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int r = m / p.group, g = m - r * p.group;
-        __nv_bfloat16* at = out + r * p.o_r + (kv_head * p.group + g) * p.o_h;
+        __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h;
 #pragma unroll
         for (int c = 0; c < D; c += 8) {
-          const uint4 x = make_uint4(pair(o[c] * inv, o[c + 1] * inv), pair(o[c + 2] * inv, o[c + 3] * inv),
+          const uint4 y = make_uint4(pair(o[c] * inv, o[c + 1] * inv), pair(o[c + 2] * inv, o[c + 3] * inv),
                                      pair(o[c + 4] * inv, o[c + 5] * inv), pair(o[c + 6] * inv, o[c + 7] * inv));
           if (wide) {
-            *(uint4*)(at + c) = x;
+            *(uint4*)(at + c) = y;
           } else {
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) ((unsigned short*)at)[c + j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
           }
         }
       }
-    } else {
-      if (holds) keep();
     }
   }
+
   if (p.split > 1) {
     cg::cluster_group cluster = cg::this_cluster();
     __syncwarp();
     cluster.sync();
     // Join the blocks' outputs: out = sum_c 2^(top_c - top) o_c / sum_c 2^(top_c - top) sum_c.  Rows are dealt out
     // over the blocks, a thread joins four columns.
-    float* parts = (float*)ring;
-    float* tops = parts + P::kRows * P::kPartRow;
-    float* sums = tops + P::kRows;
     constexpr int kD4 = D / 4;
     const bool wide = ((p.o_b | p.o_r | p.o_h) & 3) == 0 && ((uintptr_t)p.out & 7) == 0;
-    for (int i = tid + part * kTensorThreads; i < (m1 - m0) * kD4; i += kTensorThreads * p.split) {
+    for (int i = tid + part * C::kThreads; i < (m1 - m0) * kD4; i += C::kThreads * p.split) {
       const int row = i / kD4, d = (i - row * kD4) * 4;
       float most = -INFINITY;
       for (int c = 0; c < p.split; ++c) most = fmaxf(most, *cluster.map_shared_rank(&tops[row], c));
@@ -620,9 +637,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1)
   }
   before_sync();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kProducts) {
     after_sync();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::kColumns) : "memory");
   }
 }
 
@@ -660,11 +677,11 @@ bool encode(CUtensorMap* map, const void* at, int D, const AttentionParams& p, i
 
 struct TensorBuild {
   const void* kernel;
-  int smem, rows;
+  int smem, rows, threads, blocks, slots;
 };
-template <int D, int NT>
+template <typename C>
 TensorBuild tensor_build() {
-  return {(const void*)attention_tensor_kernel<D, NT>, Plan<D, NT>::kSmem, Plan<D, NT>::kRows};
+  return {(const void*)attention_tensor_kernel<C>, Plan<C>::kSmem, Plan<C>::kRows, C::kThreads, C::kBlocks, C::kN};
 }
 
 // What a build needs before its first launch on a device; the largest cluster it can be launched in.
@@ -682,7 +699,7 @@ int prepare_build(const TensorBuild& k, int at, int* limit) {
     int n = 0;
     e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) {
-      Launch l(dim3(16, 1, 1), kTensorThreads, (size_t)k.smem, nullptr, 16);
+      Launch l(dim3(16, 1, 1), (unsigned)k.threads, (size_t)k.smem, nullptr, 16);
       l.cfg.attrs = &l.at[1];  // (the cluster's size alone)
       l.cfg.numAttrs = 1;
       e = cudaOccupancyMaxActiveClusters(&n, k.kernel, &l.cfg);
@@ -698,30 +715,31 @@ int prepare_build(const TensorBuild& k, int at, int* limit) {
 
 int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st) {
   if ((p.dim != 64 && p.dim != 128) || p.page_size % 8 || !encode_function()) return ERSD_EUNSUPPORTED;
+  const int many = (int64_t)p.R * p.group > 128;
+  const TensorBuild k = p.dim == 64 ? (many ? tensor_build<Many<64>>() : tensor_build<Few<64>>())
+                                    : (many ? tensor_build<Many<128>>() : tensor_build<Few<128>>());
   int box = 8;
-  while (box < 128 && p.page_size % (box * 2) == 0) box *= 2;
+  while (box < k.slots && p.page_size % (box * 2) == 0) box *= 2;
   CUtensorMap k_map, v_map;
   if (!encode(&k_map, p.k, p.dim, p, p.k_token, p.k_head, p.k_page, box) || !encode(&v_map, p.v, p.dim, p, p.v_token, p.v_head, p.v_page, box))
     return ERSD_EUNSUPPORTED;
-  const int two = (int64_t)p.R * p.group > 128;
-  const TensorBuild k = p.dim == 64 ? (two ? tensor_build<64, 2>() : tensor_build<64, 1>()) : (two ? tensor_build<128, 2>() : tensor_build<128, 1>());
   int limit = 8;
-  const int status = prepare_build(k, (p.dim == 64 ? 0 : 2) + two, &limit);
+  const int status = prepare_build(k, (p.dim == 64 ? 0 : 2) + many, &limit);
   if (status != ERSD_OK) return status;
   p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   if (!p.split) {
-    // as many blocks as SMs, with a tile of keys at least for each
+    // as many blocks as fit on the SMs, with a tile of keys at least for each
     const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
     int64_t reach = (int64_t)max_context + p.R;
     if (p.window && reach > (int64_t)p.window + p.sinks + p.R) reach = (int64_t)p.window + p.sinks + p.R;
-    const int64_t tiles = (reach + kN - 1) / kN;
+    const int64_t tiles = (reach + k.slots - 1) / k.slots;
     p.split = 1;
-    while (p.split < limit && units * p.split * 2 <= sm_count() && p.split * 2 <= tiles) p.split *= 2;
+    while (p.split < limit && units * p.split * 2 <= k.blocks * sm_count() && p.split * 2 <= tiles) p.split *= 2;
   }
   if (p.split > limit) p.split = limit;
   note_launch("attention_tensor_kernel<%d, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows, boxes of %d", p.dim, k.rows,
-              kTensorThreads, p.row_tiles * p.split, p.heads, p.B, p.split, box);
-  Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), kTensorThreads, (size_t)k.smem, st, (unsigned)p.split);
+              k.threads, p.row_tiles * p.split, p.heads, p.B, p.split, box);
+  Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), (unsigned)k.threads, (size_t)k.smem, st, (unsigned)p.split);
   void* args[] = {(void*)&p, (void*)&k_map, (void*)&v_map, (void*)&box};
   const cudaError_t e = cudaLaunchKernelExC(&l.cfg, k.kernel, args);
   return e == cudaSuccess ? ERSD_OK : cuda_fail(e);

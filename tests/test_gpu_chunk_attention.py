@@ -207,3 +207,16 @@ def test_captured_and_on_other_streams(ersd, dtype):
     replayed = outs[0].clone()
     ersd.ersd_chunk_attention(*a, outs[0])
     assert torch.equal(replayed, outs[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,Hq,parent", [(17, 16, "4x4"), (9, 8, "chain"), (40, 16, "chain")])
+def test_full_device(ersd, dtype, R, Hq, parent):
+    """As many blocks as fit on the device at once and more, of rows for one to eight warps: warps of a block run
+    ahead of one another.  The same call gives the same bits."""
+    args = make(37, R, Hq, 4, 128, 64, [(311 * b) % 1500 + 200 for b in range(37)], dtype, poison=False)
+    want = check(ersd, *args, parent=TREES[parent])
+    out = torch.empty_like(want)
+    for _ in range(40):
+        ersd.ersd_chunk_attention(*args, out, parent=TREES[parent])
+        assert torch.equal(out, want)
