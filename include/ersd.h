@@ -384,7 +384,7 @@ typedef struct ersd_chunk_opts {
   float scale;               /* attention: factor of q.k before the softmax; 0 = 1 / sqrt(head_dim) */
   const int32_t* parent;     /* HOST [R], nullable: draft tree of the rows; NULL = every row follows the one before */
   const int32_t* row_counts; /* device [B], nullable: rows of sequence b (at most R count; NULL = R).  Rows
-                                behind them are neither read nor written */
+                                behind them have no effect and are not written */
   int32_t window;            /* attention: 0, or a key is visible only if its position is > the row's - window ... */
   int32_t sinks;             /* ... or < sinks */
   int32_t max_context;       /* attention: 0, or an upper bound of context_lens: only speeds the call up */
@@ -410,7 +410,7 @@ typedef struct ersd_chunk_opts {
  *   q device [B, R, Hq, head_dim]   out device [B, R, Hq, head_dim]   of cache->dtype, not overlapping
  *   context_lens device [B] int32
  * Scores, softmax and sums are 32-bit.  bfloat16 caches with head_dim 64 or 128, page_size a multiple
- * of 8, k and v on 16-byte boundaries in every stride run on tensor cores, with the softmax weights
+ * of 4, k and v on 16-byte boundaries in every stride run on tensor cores, with the softmax weights
  * rounded to bfloat16 for the second product; the rest on 32-bit arithmetic.
  * Errors: ERSD_EINVAL (null pointers, sizes < 1, Hq not a multiple of heads, window or sinks < 0, bad
  * parent, scale not finite); ERSD_EALIGN (a pointer off its element size); ERSD_EUNSUPPORTED for

@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionPara
       const int n = i / kD4, d = (i - n * kD4) * 4, slot = start + n;
       float4 fk = make_float4(0.f, 0.f, 0.f, 0.f), fv = fk;
       if (!keys.dead(slot)) {
-        const int entry = slot / p.page_size, page = table[entry];
+        const int entry = page_of(p, slot), page = table[entry];
         if (page >= 0 && page < p.num_pages) {
           const int in_page = slot - entry * p.page_size;
           fk = four(K + page * p.k_page + in_page * p.k_token + d, p.dim - d, wide && d + 4 <= p.dim);
@@ -383,7 +383,7 @@ extern "C" int ersd_chunk_attention(const ersd_cache* cache, const void* q, void
   p.heads = c.heads;
   p.group = Hq / c.heads;
   p.dim = c.head_dim;
-  p.page_size = c.page_size;
+  set_page_size(p, c.page_size);
   p.num_pages = c.num_pages;
   p.capacity = c.max_pages * c.page_size;
   p.window = o.window;

@@ -16,12 +16,26 @@ struct AttentionParams {
   int64_t k_page, k_token, k_head, v_page, v_token, v_head;
   int B, R, heads, group, dim;
   int page_size, num_pages, capacity;  // capacity: slots of a sequence
+  uint32_t page_magic, page_shift;     // slot / page_size = slot * page_magic >> page_shift, for slots below 2^30
   int window, sinks;
   float scale_log2;                    // scale * log2(e): the softmax works in powers of two
   int row_tiles, split;
   int tree;
   uint8_t parent[ERSD_MAX_ROWS], depth[ERSD_MAX_ROWS];
 };
+
+// n / d = n * magic >> shift for n < 2^30: with 2^(l-1) < d <= 2^l and magic = (2^(30+l) + e) / d, e < d, the product is
+// off by n e / d < 2^(30+l) / d, less than the step to the next multiple.
+static inline void set_page_size(AttentionParams& p, int d) {
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  p.page_size = d;
+  p.page_magic = (uint32_t)(((1ull << (30 + l)) + (uint64_t)d - 1) / (uint64_t)d);
+  p.page_shift = (uint32_t)(30 + l);
+}
+__device__ __forceinline__ int page_of(const AttentionParams& p, int slot) {
+  return (int)((uint64_t)(uint32_t)slot * p.page_magic >> p.page_shift);
+}
 
 // The kernel of tensor-core products, where it applies to the call's types and strides (else ERSD_EUNSUPPORTED);
 // p.split = 0: chosen there.

@@ -6,8 +6,9 @@
 // weights go back there as bfloat16 over scores they came from, and the second product takes them from there.
 // Two builds:
 //   Few<D>   up to 128 packed rows (decoding, drafts), where the cache's bytes bound the call: 64 slots at a time,
-//            scores in two buffers so that the next product of scores runs during a softmax, half of an SM's shared
-//            and tensor memory, so that two blocks share an SM and one's start and end hide behind the other.
+//            scores in two buffers so that the next product of scores runs during a softmax.  Either with half of
+//            an SM's shared and tensor memory, so that two blocks share an SM and one's start and end hide behind
+//            the other, or, for calls of no more blocks than SMs, with a ring three times as long.
 //   Many<D>  256 packed rows (long chunks), where products and powers of two do: two streams of 128 rows with a
 //            softmax group each, 128 slots at a time; one's products run while the other's softmax does.
 //
@@ -33,10 +34,11 @@ namespace {
 
 constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before its output is scaled
 
-template <int D_>
+template <int D_, int kBlocks_>
 struct Few {
-  static constexpr int D = D_, kStreams = 1, kN = 64, kBuffers = 2, kStages = D == 64 ? 8 : 4;
-  static constexpr int kWarps = 4, kThreads = 192, kBlocks = 2, kColumns = 256;
+  static constexpr int D = D_, kStreams = 1, kN = 64, kBuffers = 2;
+  static constexpr int kStages = kBlocks_ == 2 ? (D == 64 ? 8 : 4) : (D == 64 ? 16 : 12);
+  static constexpr int kWarps = 4, kThreads = 192, kBlocks = kBlocks_, kColumns = 256;
 };
 template <int D_>
 struct Many {
@@ -49,12 +51,13 @@ struct Many {
 constexpr int kTableRing = 8;  // tiles whose table entries are on their way or in use
 
 struct Misc {  // behind the ring
-  uint64_t full[12], empty[12];  // of the ring's stages
+  uint64_t full[16], empty[16];  // of the ring's stages
   uint64_t scores[2];            // of a stream (or a buffer) are in tensor memory
   uint64_t weights[2];           // and the weights that take their place.  (A buffer's own: with one barrier for both
                                  // a quick warp's next tile would count for a slow warp's last.)
   uint64_t rest[2];              // a stream's output is at rest: the product with the last weights is done
   uint64_t done;                 // all products
+  uint64_t q_there;              // q's rows are in shared memory
   uint32_t tmem;
   uint32_t gave_up;              // a wait ran out: nothing that follows it can be trusted
   int32_t entries[kTableRing][32];
@@ -214,28 +217,9 @@ __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   return (0xFFFFFFFFu >> (32 - (b - a))) << a;
 }
 
-// The order in which the ring is filled is the order of use: the keys of the first kBuffers tiles, then by tile its
-// values and the keys of the tile kBuffers on.
-template <int kBuffers>
-struct Order {
-  int tiles;
-  __device__ __forceinline__ int items() const { return 2 * tiles; }
-  __device__ __forceinline__ int keys_of(int t) const { return t < kBuffers ? t : min(tiles, kBuffers) + 2 * (t - kBuffers) + 1; }
-  __device__ __forceinline__ int values_of(int t) const { return min(tiles, kBuffers) + t + min(t, max(tiles - kBuffers, 0)); }
-  // item q: its tile; whether it is values
-  __device__ __forceinline__ int tile(int q, bool* values) const {
-    const int first = min(tiles, kBuffers);
-    *values = false;
-    if (q < first) return q;
-    const int x = q - first, both = 2 * max(tiles - kBuffers, 0);
-    if (x < both) {
-      *values = !(x & 1);
-      return (x >> 1) + (x & 1) * kBuffers;
-    }
-    *values = true;
-    return (both >> 1) + x - both;
-  }
-};
+// The ring is filled in the order of use: the keys of the first `buffers` tiles, then by tile its values and the keys
+// of the tile `buffers` on.  The place of tile t's values in that order:
+__device__ __forceinline__ int values_of(int tiles, int buffers, int t) { return min(tiles, buffers) + t + min(t, max(tiles - buffers, 0)); }
 
 template <typename C>
 __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
@@ -254,25 +238,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   const int kv_head = blockIdx.y, b = blockIdx.z;
   const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
 
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  int rows = p.row_counts ? p.row_counts[b] : p.R;
-  const int ctx = max(0, p.context_lens[b]);
-  rows = max(0, min(rows, p.R));
-  const int m0 = tile * P::kRows, m1 = min(m0 + P::kRows, rows * p.group);
-  if (m0 >= m1) return;  // (the same for every block of the cluster)
-  const int r0 = m0 / p.group, r1 = (m1 - 1) / p.group + 1;
-  // warps of each stream with rows
-  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
-  int min_depth = r0;
-  if (p.tree) {
-    min_depth = p.depth[r0];
-    for (int r = r0 + 1; r < r1; ++r) min_depth = min(min_depth, (int)p.depth[r]);
-  }
-  const KeyRange keys = key_range<kN>(p, ctx, r1, min_depth);
-  const int t0 = (int)((int64_t)keys.tiles * part / p.split), t1 = (int)((int64_t)keys.tiles * (part + 1) / p.split);
-  const Order<kBuffers> order{t1 - t0};
-  const int tiles = t1 - t0;
-
+  // ---- what needs nothing of the kernel before this one on the stream
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       barrier_init(&sh.full[i], 1);
@@ -280,12 +246,13 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     }
     for (int s = 0; s < 2; ++s) {
       barrier_init(&sh.scores[s], 1);
-      barrier_init(&sh.weights[s], (uint32_t)max(1, s && kStreams == 2 ? warps1 : warps0));
       barrier_init(&sh.rest[s], 1);
     }
     barrier_init(&sh.done, 1);
+    barrier_init(&sh.q_there, C::kWarps);
     sh.gave_up = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
   if (warp == kProducts) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&sh.tmem)), "n"(C::kColumns) : "memory");
@@ -296,30 +263,54 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       sh.parent[n] = p.parent[n];
       sh.depth[n] = p.depth[n];
     }
-  if (tid < kSoftmaxThreads) {
-    // the rows of q in the operand's layout; rows that are not there stay as they are: their scores go nowhere
-    const __nv_bfloat16* q = (const __nv_bfloat16*)p.q + b * p.q_b;
-    const bool wide = ((p.q_b | p.q_r | p.q_h) & 7) == 0 && ((uintptr_t)p.q & 15) == 0;
-    const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the softmax takes a positive scale)
-    constexpr int kPieces = D / 8;
-    for (int i = tid; i < (m1 - m0) * kPieces; i += kSoftmaxThreads) {
-      const int m = i / kPieces, c = i % kPieces, r = (m0 + m) / p.group, g = m0 + m - r * p.group;
-      const __nv_bfloat16* at = q + r * p.q_r + (kv_head * p.group + g) * p.q_h + c * 8;
-      uint4 x;
-      if (wide) {
-        x = *(const uint4*)at;
-      } else {
-        const unsigned short* e = (const unsigned short*)at;
-        x = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
-      }
-      x.x ^= flip;
-      x.y ^= flip;
-      x.z ^= flip;
-      x.w ^= flip;
-      const int row = m & 127;
-      *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kQPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- q's rows are asked for while the lengths are on their way
+  const int m0 = tile * P::kRows;
+  const __nv_bfloat16* q = (const __nv_bfloat16*)p.q + b * p.q_b;
+  const bool q_wide = ((p.q_b | p.q_r | p.q_h) & 7) == 0 && ((uintptr_t)p.q & 15) == 0;
+  const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the softmax takes a positive scale)
+  constexpr int kPieces = D / 8, kEarly = 4;  // of a row, of 16 bytes; asked for early by a thread
+  auto load_q = [&](int i) {
+    const int m = i / kPieces, c = i % kPieces, r = (m0 + m) / p.group, g = m0 + m - r * p.group;
+    const __nv_bfloat16* at = q + r * p.q_r + (kv_head * p.group + g) * p.q_h + c * 8;
+    if (q_wide) return *(const uint4*)at;
+    const unsigned short* e = (const unsigned short*)at;
+    return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+  };
+  auto store_q = [&](int i, const uint4& x) {  // in the operand's layout
+    const int m = i / kPieces, c = i % kPieces, row = m & 127;
+    *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kQPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+        make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+  };
+  uint4 early[kEarly];
+  const int most = (min(m0 + P::kRows, p.R * p.group) - m0) * kPieces;
+  if (warp < C::kWarps) {
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j)
+      if (tid + j * kSoftmaxThreads < most) early[j] = load_q(tid + j * kSoftmaxThreads);
+  }
+
+  int rows = p.row_counts ? p.row_counts[b] : p.R;
+  const int ctx = max(0, p.context_lens[b]);
+  rows = max(0, min(rows, p.R));
+  const int m1 = max(m0, min(m0 + P::kRows, rows * p.group));  // (no rows: the same for every block of the cluster)
+  const int r0 = m0 / p.group, r1 = max(r0, (m1 - 1) / p.group + 1);
+  // warps of each stream with rows
+  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
+  int min_depth = r0;
+  if (p.tree && m1 > m0) {
+    min_depth = p.depth[r0];
+    for (int r = r0 + 1; r < r1; ++r) min_depth = min(min_depth, (int)p.depth[r]);
+  }
+  const KeyRange keys = key_range<kN>(p, ctx, r1, min_depth);
+  const int all_tiles = m1 > m0 ? keys.tiles : 0;
+  const int t0 = (int)((int64_t)all_tiles * part / p.split), t1 = (int)((int64_t)all_tiles * (part + 1) / p.split);
+  const int tiles = t1 - t0;
+  if (tid == 0) {
+    for (int s = 0; s < 2; ++s) barrier_init(&sh.weights[s], (uint32_t)max(1, s && kStreams == 2 ? warps1 : warps0));
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   before_sync();
   __syncthreads();
@@ -341,48 +332,63 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   if (warp >= C::kWarps) {
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersOthers));
     if (warp == kCopies) {
-      // ---- copies: a lane has one box (`box` slots by 64 elements) of every item.  Its entries of the block table
-      // come through shared memory, so that no register waits for them.
-      const int boxes = kN / box, group = lane % boxes, panel = lane / boxes;
-      const bool mine = panel < D / 64;
+      // ---- copies: a lane has a box or two (`box` slots by 64 elements) of every item.  The entries of the block
+      // table come through shared memory, so that no register waits for them.
+      const int groups = kN / box, boxes = groups * (D / 64), shift = __ffs(groups) - 1;
+      const int group = lane & (groups - 1), panel = lane >> shift;  // of the lane's first box; a second one is 32 boxes on
       const int32_t* table = p.table + b * p.table_stride;
-      auto slot_of = [&](int t) { return tile_start<kN>(keys, t0 + t) + group * box; };
-      auto needs = [&](int slot) { return mine && slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo); };
+      auto needs = [&](int slot) { return slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo); };
       auto ask = [&](int t) {
-        if (t < tiles) {
-          const int slot = slot_of(t);
-          if (needs(slot)) copy_entry(&sh.entries[t % kTableRing][lane], table + slot / p.page_size);
+        if (t < tiles && lane < groups) {
+          const int slot = tile_start<kN>(keys, t0 + t) + lane * box;
+          if (needs(slot)) copy_entry(&sh.entries[t % kTableRing][lane], table + page_of(p, slot));
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
       constexpr int kAhead = kTableRing - kBuffers - 1;  // (a tile's values come kBuffers tiles after its keys)
 #pragma unroll
       for (int t = 0; t < kAhead; ++t) ask(t);
-      int q = 0;
-      for (; q < order.items(); ++q) {
-        const int stage = q % kStages;
-        bool values;
-        const int t = order.tile(q, &values), slot = slot_of(t);
-        const bool needed = needs(slot);
-        if (!values) {
-          ask(t + kAhead);
-          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+      int stage = 0, filled = 0;
+      uint32_t parity = 1;  // of the ring's round before: nothing to wait for in the first
+      auto fill = [&](int t, const CUtensorMap* map) {
+        const int start = tile_start<kN>(keys, t0 + t);
+        uint64_t* full = &sh.full[stage];
+        char* to = ring + stage * P::kStageBytes;
+        if (filled >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], parity, gave_up))) return false;
+        const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, lane < groups && needs(start + lane * box))) * (D / 64);
+        if (lane == 0) barrier_expect(full, count * (uint32_t)box * 128u);
+        __syncwarp();
+        for (int i = lane, g = group, c = panel; i < boxes; i += 32, g = i & (groups - 1), c = i >> shift) {
+          const int slot = start + g * box;
+          if (!needs(slot)) continue;
+          const int page = sh.entries[t % kTableRing][g];  // (outside the cache: such a page gives zeros)
+          tma_box(smem_address(to + c * kPanel + g * box * 128), map, c * 64, slot - page_of(p, slot) * p.page_size, kv_head,
+                  page < 0 || page >= p.num_pages ? p.num_pages : page, full);
         }
-        const int page = needed ? sh.entries[t % kTableRing][lane] : 0;
-        if (q >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], (uint32_t)(q / kStages - 1) & 1, gave_up))) break;
-        const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, needed));
-        if (lane == 0) barrier_expect(&sh.full[stage], count * (uint32_t)box * 128u);
         __syncwarp();
-        // (page numbers outside the cache give zeros)
-        if (needed)
-          tma_box(smem_address(ring + stage * P::kStageBytes + panel * kPanel + group * box * 128), values ? &v_map : &k_map, panel * 64,
-                  slot % p.page_size, kv_head, page < 0 || page >= p.num_pages ? p.num_pages : page, &sh.full[stage]);
+        ++filled;
+        if (++stage == kStages) {
+          stage = 0;
+          parity ^= 1;
+        }
+        return true;
+      };
+      auto fill_keys = [&](int t) {
+        ask(t + kAhead);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
         __syncwarp();
+        return fill(t, &k_map);
+      };
+      bool ok = true;
+      for (int t = 0; ok && t < kBuffers && t < tiles; ++t) ok = fill_keys(t);
+      for (int t = 0; ok && t < tiles; ++t) {
+        ok = fill(t, &v_map);
+        if (ok && t + kBuffers < tiles) ok = fill_keys(t + kBuffers);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       // every copy has landed before the block ends, even where the products gave up
       if (*(volatile uint32_t*)gave_up)
-        for (int x = max(0, q - kStages); x < q; ++x)
+        for (int x = max(0, filled - kStages); x < filled; ++x)
           for (int i = 0; i < (1 << 22) && !barrier_try(&sh.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
           }
       __syncwarp();
@@ -391,37 +397,50 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       if (lane == 0 && tiles > 0) {
         constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
         const int streams = kStreams == 2 && warps1 > 0 ? 2 : 1;
-        bool ok = true;
-        auto wait_item = [&](int q) { return barrier_wait(&sh.full[q % kStages], (uint32_t)(q / kStages) & 1, gave_up); };
-        auto score = [&](int s, int t) {  // scores of stream s with tile t
-          const int item = order.keys_of(t), buffer = kBuffers == 2 ? t & 1 : s;
-          if (!wait_item(item)) return false;
-          after_sync();
-          const uint32_t a = smem_address(q_tile) + s * 128 * D * 2, k = smem_address(ring + (item % kStages) * P::kStageBytes);
-#pragma unroll
-          for (int j = 0; j < D / 16; ++j)
-            mma_shared(tmem + buffer * kN, operand(a + (j >> 2) * kQPanel + (j & 3) * 32, 16), operand(k + (j >> 2) * kPanel + (j & 3) * 32, 16),
-                       kScores, j > 0);
-          mma_commit(&sh.scores[buffer]);
-          if (s == streams - 1) mma_commit(&sh.empty[item % kStages]);
+        // items come in the order of use: the ring's place of the next one, and of the last keys and values
+        int stage = 0;
+        uint32_t parity = 0;
+        const uint64_t q_operand = operand(smem_address(q_tile), 16), ring_keys = operand(smem_address(ring), 16),
+                       ring_values = operand(smem_address(ring), kPanel);
+        auto next_item = [&](int* at) {
+          if (!barrier_wait(&sh.full[stage], parity, gave_up)) return false;
+          *at = stage;
+          if (++stage == kStages) {
+            stage = 0;
+            parity ^= 1;
+          }
           return true;
         };
+        int keys_at = 0, values_at = 0;
+        auto score = [&](int s, int t) {  // scores of stream s with tile t
+          const int buffer = kBuffers == 2 ? t & 1 : s;
+          if (s == 0 && !next_item(&keys_at)) return false;
+          after_sync();
+          // (addresses are in steps of 16 bytes in an operand's lowest bits)
+          const uint64_t a = q_operand + (uint32_t)(s * (128 * D * 2 >> 4)), k = ring_keys + (uint32_t)(keys_at * (P::kStageBytes >> 4));
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+            mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4), k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4),
+                       kScores, j > 0);
+          mma_commit(&sh.scores[buffer]);
+          if (s == streams - 1) mma_commit(&sh.empty[keys_at]);
+          return true;
+        };
+        bool ok = barrier_wait(&sh.q_there, 0, gave_up);
         for (int t = 0; ok && t < kBuffers && t < tiles; ++t)
           for (int s = 0; ok && s < streams; ++s) ok = score(s, t);
         for (int t = 0; ok && t < tiles; ++t)
           for (int s = 0; ok && s < streams; ++s) {
-            const int item = order.values_of(t), buffer = kBuffers == 2 ? t & 1 : s;
-            ok = barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up);
-            if (!ok) break;
-            ok = wait_item(item);
-            if (!ok) break;
+            const int buffer = kBuffers == 2 ? t & 1 : s;
+            if (s == 0) ok = next_item(&values_at);
+            if (!ok || !(ok = barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up))) break;
             after_sync();
-            const uint32_t v = smem_address(ring + (item % kStages) * P::kStageBytes);
+            const uint64_t v = ring_values + (uint32_t)(values_at * (P::kStageBytes >> 4));
 #pragma unroll
             for (int j = 0; j < kN / 16; ++j)
-              mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, operand(v + j * 16 * 128, kPanel), kOutput, t > 0 || j > 0);
+              mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, v + (uint32_t)(j * 16 * 128 >> 4), kOutput, t > 0 || j > 0);
             if (kBuffers == 2) mma_commit(&sh.rest[s]);
-            if (s == streams - 1) mma_commit(&sh.empty[item % kStages]);
+            if (s == streams - 1) mma_commit(&sh.empty[values_at]);
             if (t + kBuffers < tiles) ok = score(s, t + kBuffers);
           }
         mma_commit(&sh.done);
@@ -432,6 +451,16 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   } else {
     // ---- softmax: a thread has one row
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersSoftmax));
+    {  // rows of q that are not there stay as they are: their scores go nowhere
+      const int pieces = (m1 - m0) * kPieces;
+#pragma unroll
+      for (int j = 0; j < kEarly; ++j)
+        if (tid + j * kSoftmaxThreads < pieces) store_q(tid + j * kSoftmaxThreads, early[j]);
+      for (int i = tid + kEarly * kSoftmaxThreads; i < pieces; i += kSoftmaxThreads) store_q(i, load_q(i));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) barrier_arrive(&sh.q_there);
+    }
     const int s = warp >> 2, quarter = warp & 3;
     const int row = quarter * 32 + lane, m = m0 + s * 128 + row;
     const int my_warps = s ? warps1 : warps0;
@@ -484,7 +513,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           bool any_dead = keys.dead(start) || keys.dead(start + kN - 1);
           if (!any_dead) any_dead = keys.sink_hi < keys.lo && keys.sink_hi < start + kN && keys.lo > start;
           if (any_dead) {
-            const int item = order.values_of(t);
+            const int item = values_of(tiles, kBuffers, t);
             if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.full[item % kStages], (uint32_t)(item / kStages) & 1, gave_up))) break;
             // the stream's warps share the tile's rows
             for (int n = row; n < kN; n += my_warps * 32)
@@ -599,27 +628,46 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     __syncwarp();
     cluster.sync();
     // Join the blocks' outputs: out = sum_c 2^(top_c - top) o_c / sum_c 2^(top_c - top) sum_c.  Rows are dealt out
-    // over the blocks, a thread joins four columns.
-    constexpr int kD4 = D / 4;
+    // over the cluster's warps; lane c works out block c's factor, then a lane joins four columns (or, where a head
+    // has 64, half a warp a row's half of the blocks).
+    constexpr int kD4 = D / 4, kGroups = 32 / kD4;
     const bool wide = ((p.o_b | p.o_r | p.o_h) & 3) == 0 && ((uintptr_t)p.out & 7) == 0;
-    for (int i = tid + part * C::kThreads; i < (m1 - m0) * kD4; i += C::kThreads * p.split) {
-      const int row = i / kD4, d = (i - row * kD4) * 4;
-      float most = -INFINITY;
-      for (int c = 0; c < p.split; ++c) most = fmaxf(most, *cluster.map_shared_rank(&tops[row], c));
-      if (most == -INFINITY) most = 0.f;
-      float total = 0.f;
-      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int c = 0; c < p.split; ++c) {
-        const float theirs = *cluster.map_shared_rank(&sums[row], c);
-        if (theirs == 0.f) continue;
-        const float f = power_of_two(*cluster.map_shared_rank(&tops[row], c) - most);
-        const float4 x = *(const float4*)cluster.map_shared_rank(&parts[row * P::kPartRow + d], c);
-        total = fmaf(f, theirs, total);
-        y.x = fmaf(f, x.x, y.x);
-        y.y = fmaf(f, x.y, y.y);
-        y.z = fmaf(f, x.z, y.z);
-        y.w = fmaf(f, x.w, y.w);
+    for (int row = warp * p.split + part; row < m1 - m0; row += (C::kThreads / 32) * p.split) {
+      float their_top = -INFINITY, their_sum = 0.f;
+      if (lane < p.split) {
+        their_top = *cluster.map_shared_rank(&tops[row], lane);
+        their_sum = *cluster.map_shared_rank(&sums[row], lane);
       }
+      float most = their_top;
+#pragma unroll
+      for (int w = 8; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, w));
+      if (most == -INFINITY) most = 0.f;
+      float f = lane < p.split && their_sum != 0.f ? power_of_two(their_top - most) : 0.f;  // (0: saw nothing)
+      float total = f != 0.f || their_sum != their_sum ? f * their_sum : 0.f;
+#pragma unroll
+      for (int w = 8; w; w >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, w);
+      total = __shfl_sync(0xFFFFFFFFu, total, 0);  // (lanes 0 to 15 hold the sum)
+      const int d = (lane % kD4) * 4, first = lane / kD4;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int c0 = 0; c0 < p.split; c0 += kGroups) {
+        const int c = c0 + first;
+        const float g = __shfl_sync(0xFFFFFFFFu, f, c & 31);
+        if (c < p.split && g != 0.f) {
+          const float4 x = *(const float4*)cluster.map_shared_rank(&parts[row * P::kPartRow + d], c);
+          y.x = fmaf(g, x.x, y.x);
+          y.y = fmaf(g, x.y, y.y);
+          y.z = fmaf(g, x.z, y.z);
+          y.w = fmaf(g, x.w, y.w);
+        }
+      }
+      if (kGroups == 2) {
+        y.x += __shfl_xor_sync(0xFFFFFFFFu, y.x, 16);
+        y.y += __shfl_xor_sync(0xFFFFFFFFu, y.y, 16);
+        y.z += __shfl_xor_sync(0xFFFFFFFFu, y.z, 16);
+        y.w += __shfl_xor_sync(0xFFFFFFFFu, y.w, 16);
+      }
+      if (first) continue;
       const float inv = total == 0.f ? 0.f : 1.f / total;
       const int r = (m0 + row) / p.group, g = m0 + row - r * p.group;
       __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h + d;
@@ -684,59 +732,66 @@ TensorBuild tensor_build() {
   return {(const void*)attention_tensor_kernel<C>, Plan<C>::kSmem, Plan<C>::kRows, C::kThreads, C::kBlocks, C::kN};
 }
 
-// What a build needs before its first launch on a device; the largest cluster it can be launched in.
-int prepare_build(const TensorBuild& k, int at, int* limit) {
+// What a build needs before its first launch on a device; clusters[i]: how many clusters of 2^i blocks, i <= 4, the
+// device holds at a time.
+int prepare_build(const TensorBuild& k, int at, const int** clusters) {
   static std::mutex m;
-  static int known[4][64];
+  static int known[6][64][5];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(e);
   if (dev < 0 || dev >= 64) return ERSD_EUNSUPPORTED;
   std::lock_guard<std::mutex> lock(m);
-  if (!known[at][dev]) {
+  int* n = known[at][dev];
+  if (!n[0]) {
     e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
     if (e != cudaSuccess) return cuda_fail(e);
-    int n = 0;
-    e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) {
-      Launch l(dim3(16, 1, 1), (unsigned)k.threads, (size_t)k.smem, nullptr, 16);
+    (void)cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    for (int i = 1; i <= 4; ++i) {
+      Launch l(dim3(1u << i, 1, 1), (unsigned)k.threads, (size_t)k.smem, nullptr, 1u << i);
       l.cfg.attrs = &l.at[1];  // (the cluster's size alone)
       l.cfg.numAttrs = 1;
-      e = cudaOccupancyMaxActiveClusters(&n, k.kernel, &l.cfg);
+      if (cudaOccupancyMaxActiveClusters(&n[i], k.kernel, &l.cfg) != cudaSuccess) n[i] = 0;
     }
-    (void)cudaGetLastError();  // a refused opt-in only means clusters of eight
-    known[at][dev] = e == cudaSuccess && n >= 1 ? 16 : 8;
+    (void)cudaGetLastError();  // a size that is refused fits no time
+    n[0] = 1;
   }
-  *limit = known[at][dev];
+  *clusters = n;
   return ERSD_OK;
 }
 
 }  // namespace
 
 int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st) {
-  if ((p.dim != 64 && p.dim != 128) || p.page_size % 8 || !encode_function()) return ERSD_EUNSUPPORTED;
-  const int many = (int64_t)p.R * p.group > 128;
-  const TensorBuild k = p.dim == 64 ? (many ? tensor_build<Many<64>>() : tensor_build<Few<64>>())
-                                    : (many ? tensor_build<Many<128>>() : tensor_build<Few<128>>());
-  int box = 8;
+  if ((p.dim != 64 && p.dim != 128) || p.page_size % 4 || !encode_function()) return ERSD_EUNSUPPORTED;
+  const int64_t sms = sm_count();
+  const bool many = (int64_t)p.R * p.group > 128;
+  p.row_tiles = (int)(((int64_t)p.R * p.group + (many ? 255 : 127)) / (many ? 256 : 128));
+  const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
+  // Blocks with a long ring while no more than one goes to an SM (one token over 64000 positions: XX against 107 us),
+  // else two to an SM.
+  const bool alone = many || units * (p.split ? p.split : 1) <= sms;
+  const int at = (p.dim == 64 ? 0 : 3) + (many ? 2 : alone ? 1 : 0);
+  const TensorBuild builds[6] = {tensor_build<Few<64, 2>>(),  tensor_build<Few<64, 1>>(),  tensor_build<Many<64>>(),
+                                 tensor_build<Few<128, 2>>(), tensor_build<Few<128, 1>>(), tensor_build<Many<128>>()};
+  const TensorBuild& k = builds[at];
+  int box = 4;
   while (box < k.slots && p.page_size % (box * 2) == 0) box *= 2;
   CUtensorMap k_map, v_map;
   if (!encode(&k_map, p.k, p.dim, p, p.k_token, p.k_head, p.k_page, box) || !encode(&v_map, p.v, p.dim, p, p.v_token, p.v_head, p.v_page, box))
     return ERSD_EUNSUPPORTED;
-  int limit = 8;
-  const int status = prepare_build(k, (p.dim == 64 ? 0 : 2) + many, &limit);
+  const int* clusters;
+  const int status = prepare_build(k, at, &clusters);
   if (status != ERSD_OK) return status;
-  p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   if (!p.split) {
-    // as many blocks as fit on the SMs, with a tile of keys at least for each
-    const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
+    // as many blocks as SMs, with a tile of keys at least for each, and no cluster that has to wait for another
     int64_t reach = (int64_t)max_context + p.R;
     if (p.window && reach > (int64_t)p.window + p.sinks + p.R) reach = (int64_t)p.window + p.sinks + p.R;
     const int64_t tiles = (reach + k.slots - 1) / k.slots;
     p.split = 1;
-    while (p.split < limit && units * p.split * 2 <= k.blocks * sm_count() && p.split * 2 <= tiles) p.split *= 2;
+    for (int i = 1; i <= 4 && units << i <= sms && 1 << i <= tiles && units <= clusters[i]; ++i) p.split = 1 << i;
   }
-  if (p.split > limit) p.split = limit;
+  while (p.split > 1 && !clusters[__builtin_ctz(p.split)]) p.split /= 2;
   note_launch("attention_tensor_kernel<%d, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows, boxes of %d", p.dim, k.rows,
               k.threads, p.row_tiles * p.split, p.heads, p.B, p.split, box);
   Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), (unsigned)k.threads, (size_t)k.smem, st, (unsigned)p.split);
