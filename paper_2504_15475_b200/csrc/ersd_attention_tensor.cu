@@ -1,7 +1,7 @@
 // ersd_chunk_attention on tensor cores: bfloat16 caches with heads of 64 or 128.
 //
-// A thread block takes a tile of packed rows of one kv head (see AttentionParams) through its keys.  One warp
-// copies keys and values page by page with TMA into a ring of shared memory, one thread issues the products
+// A thread block takes a tile of packed rows of one kv head (see AttentionParams) through its keys.  A warp each
+// copies keys and values page by page with TMA into rings of shared memory, another issues the products
 // (tcgen05.mma), and groups of four warps do the softmax, a thread to a row: scores come out of tensor memory,
 // weights go back there as bfloat16 over scores they came from, and the second product takes them from there.
 // Two builds:
@@ -37,21 +37,26 @@ constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before 
 template <int D_, int kBlocks_>
 struct Few {
   static constexpr int D = D_, kStreams = 1, kN = 64, kBuffers = 2;
-  static constexpr int kStages = kBlocks_ == 2 ? (D == 64 ? 8 : 4) : (D == 64 ? 16 : 12);
-  static constexpr int kWarps = 4, kThreads = 192, kBlocks = kBlocks_, kColumns = 256;
+  static constexpr int kKeyStages = kBlocks_ == 2 ? (D == 64 ? 4 : 2) : (D == 64 ? 8 : 6), kValueStages = kKeyStages;
+  static constexpr int kWarps = 4, kThreads = 256, kBlocks = kBlocks_, kColumns = 256;
 };
 template <int D_>
 struct Many {
-  static constexpr int D = D_, kStreams = 2, kN = 128, kBuffers = 1, kStages = D == 64 ? 12 : 5;
-  // (two warps without work make the last four a group that gives its registers to the others)
+  static constexpr int D = D_, kStreams = 2, kN = 128, kBuffers = 1;
+  static constexpr int kKeyStages = D == 64 ? 6 : 3, kValueStages = D == 64 ? 6 : 2;
+  // (the last four warps are a group that gives its registers to the others)
   static constexpr int kWarps = 8, kThreads = 384, kBlocks = 1, kColumns = 512;
-  static constexpr int kRegistersSoftmax = 216, kRegistersOthers = 72;  // 2 * 216 + 72 = 3 * 168, what a launch gives
+  static constexpr int kRegistersSoftmax = 200, kRegistersOthers = 104;  // 2 * 200 + 104 = 3 * 168, what a launch gives
 };
 
 constexpr int kTableRing = 8;  // tiles whose table entries are on their way or in use
 
-struct Misc {  // behind the ring
-  uint64_t full[16], empty[16];  // of the ring's stages
+struct Ring {  // of keys or values
+  uint64_t full[8], empty[8];
+  int32_t entries[kTableRing][32];
+};
+struct Misc {  // behind the rings
+  Ring ring[2];                  // keys, values
   uint64_t scores[2];            // of a stream (or a buffer) are in tensor memory
   uint64_t weights[2];           // and the weights that take their place.  (A buffer's own: with one barrier for both
                                  // a quick warp's next tile would count for a slow warp's last.)
@@ -60,18 +65,17 @@ struct Misc {  // behind the ring
   uint64_t q_there;              // q's rows are in shared memory
   uint32_t tmem;
   uint32_t gave_up;              // a wait ran out: nothing that follows it can be trusted
-  int32_t entries[kTableRing][32];
   uint8_t parent[ERSD_MAX_ROWS], depth[ERSD_MAX_ROWS];
 };
-static_assert(sizeof(Misc) <= 2048, "");
+static_assert(sizeof(Misc) <= 3072, "");
 
 template <typename C>
 struct Plan : C {
-  static constexpr int D = C::D, kN = C::kN, kStages = C::kStages;
+  static constexpr int D = C::D, kN = C::kN, kStages = C::kKeyStages + C::kValueStages;
   static constexpr int kRows = C::kStreams * 128;
   static constexpr int kStageBytes = kN * D * 2;  // keys or values of a tile
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes + 2048;
+  static constexpr int kSmem = kQBytes + kStages * kStageBytes + 3072;
   static constexpr int kOutputs = C::kStreams * C::kBuffers * kN;  // first column of the outputs
   static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
   static_assert(kRows * (kPartRow + 2) * 4 <= kQBytes + kStages * kStageBytes, "");
@@ -104,15 +108,21 @@ __device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Whether the phase ended; false when it did not within some seconds, or another wait of the block ran out.
+// For a whole warp: whether the phase ended; false when it did not within some seconds, or another wait of the block
+// ran out.  (The vote keeps the warp together, and tells the compiler so: what one thread issues later comes from
+// registers that the warp shares.)
 __device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, uint32_t* gave_up) {
-  if (barrier_try(b, parity)) return true;
   for (int i = 0; i < (1 << 22); ++i) {
-    if (barrier_try(b, parity)) return true;
-    if (*(volatile uint32_t*)gave_up) return false;
+    if (__all_sync(0xFFFFFFFFu, barrier_try(b, parity))) return true;
+    if (__any_sync(0xFFFFFFFFu, *(volatile uint32_t*)gave_up != 0)) return false;
   }
   *(volatile uint32_t*)gave_up = 1;
   return false;
+}
+__device__ __forceinline__ bool elected() {  // one thread of the warp
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
 }
 
 __device__ __forceinline__ void tma_box(uint32_t to, const CUtensorMap* map, int x, int token, int head, int page, uint64_t* full) {
@@ -162,11 +172,16 @@ __device__ __forceinline__ void tmem_load(uint32_t at, uint32_t* r) {
       : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24)
       : "r"(at));
 }
-__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
+__device__ __forceinline__ void tmem_load_16(uint32_t at, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::S8(r, 0),
-      S8(r, 8), S8(r, 16), S8(r, 24), "r"(at)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : R8(r, 0), R8(r, 8)
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_store_16(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::S8(r, 0),
+      S8(r, 8), "r"(at)
       : "memory");
 }
 __device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -217,40 +232,37 @@ __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   return (0xFFFFFFFFu >> (32 - (b - a))) << a;
 }
 
-// The ring is filled in the order of use: the keys of the first `buffers` tiles, then by tile its values and the keys
-// of the tile `buffers` on.  The place of tile t's values in that order:
-__device__ __forceinline__ int values_of(int tiles, int buffers, int t) { return min(tiles, buffers) + t + min(t, max(tiles - buffers, 0)); }
-
 template <typename C>
 __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     attention_tensor_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map,
                             const __grid_constant__ CUtensorMap v_map, const int box) {
   using P = Plan<C>;
-  constexpr int D = P::D, kN = P::kN, kStages = P::kStages, kStreams = C::kStreams, kBuffers = C::kBuffers;
+  constexpr int D = P::D, kN = P::kN, kStreams = C::kStreams, kBuffers = C::kBuffers;
   constexpr int kPanel = kN * 128, kQPanel = 128 * 128;  // bytes of a panel: rows of 64 elements
-  constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = C::kWarps + 1;  // (the last two: warps)
-  extern __shared__ char raw[];
-  char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  char* q_tile = base;
-  char* ring = base + P::kQBytes;
-  Misc& sh = *(Misc*)(ring + kStages * P::kStageBytes);
+  constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = C::kWarps + 2;  // (the last two: warps)
+  extern __shared__ __align__(1024) char raw[];
+  char* q_tile = raw;
+  char* key_ring = q_tile + P::kQBytes;
+  char* value_ring = key_ring + C::kKeyStages * P::kStageBytes;
+  Misc& sh = *(Misc*)(value_ring + C::kValueStages * P::kStageBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kv_head = blockIdx.y, b = blockIdx.z;
   const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
 
   // ---- what needs nothing of the kernel before this one on the stream
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      barrier_init(&sh.full[i], 1);
-      barrier_init(&sh.empty[i], 1);
-    }
+    for (int i = 0; i < 8; ++i)
+      for (int s = 0; s < 2; ++s) {
+        barrier_init(&sh.ring[s].full[i], 1);
+        barrier_init(&sh.ring[s].empty[i], 1);
+      }
     for (int s = 0; s < 2; ++s) {
       barrier_init(&sh.scores[s], 1);
       barrier_init(&sh.rest[s], 1);
     }
     barrier_init(&sh.done, 1);
     barrier_init(&sh.q_there, C::kWarps);
-    sh.gave_up = 0;
+    sh.gave_up = (smem_address(raw) & 1023) != 0;  // (the operands' layout wants it so)
     asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
@@ -318,7 +330,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   const uint32_t tmem = sh.tmem;
   uint32_t* const gave_up = &sh.gave_up;
 
-  float* parts = (float*)base;                         // [rows][kPartRow]
+  float* parts = (float*)q_tile;                        // [rows][kPartRow]
   float* tops = parts + P::kRows * P::kPartRow;        // [rows]
   float* sums = tops + P::kRows;                       // [rows]
   auto products_done = [&]() {
@@ -331,9 +343,14 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   };
   if (warp >= C::kWarps) {
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersOthers));
-    if (warp == kCopies) {
-      // ---- copies: a lane has a box or two (`box` slots by 64 elements) of every item.  The entries of the block
-      // table come through shared memory, so that no register waits for them.
+    if (warp == kCopies || warp == kCopies + 1) {
+      // ---- copies of keys, of values: a lane has a box or two (`box` slots by 64 elements) of every tile.  The entries
+      // of the block table come through shared memory, so that no register waits for them.
+      const bool values = warp != kCopies;
+      const int stages = values ? C::kValueStages : C::kKeyStages;
+      const CUtensorMap* map = values ? &v_map : &k_map;
+      char* const places = values ? value_ring : key_ring;
+      Ring& ring = sh.ring[values];
       const int groups = kN / box, boxes = groups * (D / 64), shift = __ffs(groups) - 1;
       const int group = lane & (groups - 1), panel = lane >> shift;  // of the lane's first box; a second one is 32 boxes on
       const int32_t* table = p.table + b * p.table_stride;
@@ -341,111 +358,105 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       auto ask = [&](int t) {
         if (t < tiles && lane < groups) {
           const int slot = tile_start<kN>(keys, t0 + t) + lane * box;
-          if (needs(slot)) copy_entry(&sh.entries[t % kTableRing][lane], table + page_of(p, slot));
+          if (needs(slot)) copy_entry(&ring.entries[t % kTableRing][lane], table + page_of(p, slot));
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      constexpr int kAhead = kTableRing - kBuffers - 1;  // (a tile's values come kBuffers tiles after its keys)
+      constexpr int kAhead = kTableRing - 1;
 #pragma unroll
       for (int t = 0; t < kAhead; ++t) ask(t);
-      int stage = 0, filled = 0;
+      int stage = 0, t = 0;
       uint32_t parity = 1;  // of the ring's round before: nothing to wait for in the first
-      auto fill = [&](int t, const CUtensorMap* map) {
+      for (; t < tiles; ++t) {
         const int start = tile_start<kN>(keys, t0 + t);
-        uint64_t* full = &sh.full[stage];
-        char* to = ring + stage * P::kStageBytes;
-        if (filled >= kStages && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.empty[stage], parity, gave_up))) return false;
+        uint64_t* full = &ring.full[stage];
+        ask(t + kAhead);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        if (t >= stages && !barrier_wait(&ring.empty[stage], parity, gave_up)) break;
         const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, lane < groups && needs(start + lane * box))) * (D / 64);
         if (lane == 0) barrier_expect(full, count * (uint32_t)box * 128u);
         __syncwarp();
+        const uint32_t to = smem_address(places + stage * P::kStageBytes);
         for (int i = lane, g = group, c = panel; i < boxes; i += 32, g = i & (groups - 1), c = i >> shift) {
           const int slot = start + g * box;
           if (!needs(slot)) continue;
-          const int page = sh.entries[t % kTableRing][g];  // (outside the cache: such a page gives zeros)
-          tma_box(smem_address(to + c * kPanel + g * box * 128), map, c * 64, slot - page_of(p, slot) * p.page_size, kv_head,
+          const int page = ring.entries[t % kTableRing][g];  // (outside the cache: such a page gives zeros)
+          tma_box(to + c * kPanel + g * box * 128, map, c * 64, slot - page_of(p, slot) * p.page_size, kv_head,
                   page < 0 || page >= p.num_pages ? p.num_pages : page, full);
         }
         __syncwarp();
-        ++filled;
-        if (++stage == kStages) {
+        if (++stage == stages) {
           stage = 0;
           parity ^= 1;
         }
-        return true;
-      };
-      auto fill_keys = [&](int t) {
-        ask(t + kAhead);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-        __syncwarp();
-        return fill(t, &k_map);
-      };
-      bool ok = true;
-      for (int t = 0; ok && t < kBuffers && t < tiles; ++t) ok = fill_keys(t);
-      for (int t = 0; ok && t < tiles; ++t) {
-        ok = fill(t, &v_map);
-        if (ok && t + kBuffers < tiles) ok = fill_keys(t + kBuffers);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       // every copy has landed before the block ends, even where the products gave up
       if (*(volatile uint32_t*)gave_up)
-        for (int x = max(0, filled - kStages); x < filled; ++x)
-          for (int i = 0; i < (1 << 22) && !barrier_try(&sh.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
+        for (int x = max(0, t - stages); x < t; ++x)
+          for (int i = 0; i < (1 << 22) && !barrier_try(&ring.full[x % stages], (uint32_t)(x / stages) & 1); ++i) {
           }
       __syncwarp();
     } else if (warp == kProducts) {
-      // ---- products
-      if (lane == 0 && tiles > 0) {
+      // ---- products: the warp stays together, one thread issues
+      if (tiles > 0) {
         constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
         const int streams = kStreams == 2 && warps1 > 0 ? 2 : 1;
-        // items come in the order of use: the ring's place of the next one, and of the last keys and values
-        int stage = 0;
-        uint32_t parity = 0;
-        const uint64_t q_operand = operand(smem_address(q_tile), 16), ring_keys = operand(smem_address(ring), 16),
-                       ring_values = operand(smem_address(ring), kPanel);
-        auto next_item = [&](int* at) {
-          if (!barrier_wait(&sh.full[stage], parity, gave_up)) return false;
-          *at = stage;
-          if (++stage == kStages) {
-            stage = 0;
-            parity ^= 1;
-          }
-          return true;
-        };
-        int keys_at = 0, values_at = 0;
-        auto score = [&](int s, int t) {  // scores of stream s with tile t
+        const bool leader = elected();
+        const uint64_t q_operand = operand(smem_address(q_tile), 16), key_operand = operand(smem_address(key_ring), 16),
+                       value_operand = operand(smem_address(value_ring), kPanel);
+        int key_stage = 0, value_stage = 0;
+        uint32_t key_parity = 0, value_parity = 0;
+        // Scores of stream s with tile t.  (Addresses are in steps of 16 bytes in an operand's lowest bits.)
+        auto score = [&](int s, int t) {
           const int buffer = kBuffers == 2 ? t & 1 : s;
-          if (s == 0 && !next_item(&keys_at)) return false;
+          if (s == 0 && !barrier_wait(&sh.ring[0].full[key_stage], key_parity, gave_up)) return false;
           after_sync();
-          // (addresses are in steps of 16 bytes in an operand's lowest bits)
-          const uint64_t a = q_operand + (uint32_t)(s * (128 * D * 2 >> 4)), k = ring_keys + (uint32_t)(keys_at * (P::kStageBytes >> 4));
+          const uint64_t a = q_operand + (uint32_t)(s * (128 * D * 2 >> 4)), k = key_operand + (uint32_t)(key_stage * (P::kStageBytes >> 4));
+          if (leader) {
 #pragma unroll
-          for (int j = 0; j < D / 16; ++j)
-            mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4), k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4),
-                       kScores, j > 0);
-          mma_commit(&sh.scores[buffer]);
-          if (s == streams - 1) mma_commit(&sh.empty[keys_at]);
+            for (int j = 0; j < D / 16; ++j)
+              mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4),
+                         k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4), kScores, j > 0);
+            mma_commit(&sh.scores[buffer]);
+            if (s == streams - 1) mma_commit(&sh.ring[0].empty[key_stage]);
+          }
+          __syncwarp();
+          if (s == streams - 1 && ++key_stage == C::kKeyStages) {
+            key_stage = 0;
+            key_parity ^= 1;
+          }
           return true;
         };
         bool ok = barrier_wait(&sh.q_there, 0, gave_up);
         for (int t = 0; ok && t < kBuffers && t < tiles; ++t)
           for (int s = 0; ok && s < streams; ++s) ok = score(s, t);
-        for (int t = 0; ok && t < tiles; ++t)
+        for (int t = 0; ok && t < tiles; ++t) {
           for (int s = 0; ok && s < streams; ++s) {
             const int buffer = kBuffers == 2 ? t & 1 : s;
-            if (s == 0) ok = next_item(&values_at);
-            if (!ok || !(ok = barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up))) break;
+            if (s == 0) ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up);
+            ok = ok && barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up);
+            if (!ok) break;
             after_sync();
-            const uint64_t v = ring_values + (uint32_t)(values_at * (P::kStageBytes >> 4));
+            const uint64_t v = value_operand + (uint32_t)(value_stage * (P::kStageBytes >> 4));
+            if (leader) {
 #pragma unroll
-            for (int j = 0; j < kN / 16; ++j)
-              mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, v + (uint32_t)(j * 16 * 128 >> 4), kOutput, t > 0 || j > 0);
-            if (kBuffers == 2) mma_commit(&sh.rest[s]);
-            if (s == streams - 1) mma_commit(&sh.empty[values_at]);
+              for (int j = 0; j < kN / 16; ++j)
+                mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, v + (uint32_t)(j * 16 * 128 >> 4), kOutput, t > 0 || j > 0);
+              if (kBuffers == 2) mma_commit(&sh.rest[s]);
+              if (s == streams - 1) mma_commit(&sh.ring[1].empty[value_stage]);
+            }
+            __syncwarp();
             if (t + kBuffers < tiles) ok = score(s, t + kBuffers);
           }
-        mma_commit(&sh.done);
+          if (++value_stage == C::kValueStages) {
+            value_stage = 0;
+            value_parity ^= 1;
+          }
+        }
+        if (leader) mma_commit(&sh.done);
+        __syncwarp();
       }
-      __syncwarp();
     }
     products_done();
   } else {
@@ -480,7 +491,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       for (int t = 0; t < tiles; ++t) {
         const int start = tile_start<kN>(keys, t0 + t), buffer = kBuffers == 2 ? t & 1 : s;
         const uint32_t scores = tmem + lanes + buffer * kN;
-        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.scores[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up))) break;
+        if (!barrier_wait(&sh.scores[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up)) break;
         after_sync();
         uint32_t x[kN];
 #pragma unroll
@@ -513,12 +524,11 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           bool any_dead = keys.dead(start) || keys.dead(start + kN - 1);
           if (!any_dead) any_dead = keys.sink_hi < keys.lo && keys.sink_hi < start + kN && keys.lo > start;
           if (any_dead) {
-            const int item = values_of(tiles, kBuffers, t);
-            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.full[item % kStages], (uint32_t)(item / kStages) & 1, gave_up))) break;
+            if (!barrier_wait(&sh.ring[1].full[t % C::kValueStages], (uint32_t)(t / C::kValueStages) & 1, gave_up)) break;
             // the stream's warps share the tile's rows
             for (int n = row; n < kN; n += my_warps * 32)
               if (keys.dead(start + n)) {
-                char* v = ring + (item % kStages) * P::kStageBytes + n * 128;
+                char* v = value_ring + (t % C::kValueStages) * P::kStageBytes + n * 128;
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c)
 #pragma unroll
@@ -541,38 +551,38 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           // The output has to be at rest.  (With one buffer it is: this tile's scores come after the product with the
           // last weights.)
           if (kBuffers == 2) {
-            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.rest[s], (uint32_t)(t - 1) & 1, gave_up))) break;
+            if (!barrier_wait(&sh.rest[s], (uint32_t)(t - 1) & 1, gave_up)) break;
             after_sync();
           }
           const float f = rise ? power_of_two(top - now) : 1.0f;
           sum *= f;
           if (rise) top = now;
-#pragma unroll
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            tmem_load(output + c, o);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_load_16(output + c, o);
             tmem_loaded();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_store(output + c, o);
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_store_16(output + c, o);
           }
         }
         const float minus = top == -INFINITY ? 0.f : -top;
         const uint64_t scale_two = two(scale, scale), minus_two = two(minus, minus);
         uint64_t both[2] = {0, 0};
 #pragma unroll
-        for (int half = 0; half < kN / 64; ++half) {
-          uint32_t w[32];
+        for (int c0 = 0; c0 < kN; c0 += 32) {
+          uint32_t w[16];
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) {
+          for (int c = 0; c < 32; c += 2) {
             float e0, e1;
-            apart(fma_two(two(__uint_as_float(x[half * 64 + c]), __uint_as_float(x[half * 64 + c + 1])), scale_two, minus_two), e0, e1);
+            apart(fma_two(two(__uint_as_float(x[c0 + c]), __uint_as_float(x[c0 + c + 1])), scale_two, minus_two), e0, e1);
             e0 = power_of_two(e0);
             e1 = power_of_two(e1);
             both[c >> 1 & 1] = add_two(both[c >> 1 & 1], two(e0, e1));
             w[c >> 1] = pair(e0, e1);
           }
-          tmem_store(scores + half * 32, w);
+          tmem_store_16(scores + c0 / 2, w);
         }
         float s0, s1;
         apart(add_two(both[0], both[1]), s0, s1);
@@ -587,39 +597,40 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     products_done();
     const bool wide = ((p.o_b | p.o_r | p.o_h) & 7) == 0 && ((uintptr_t)p.out & 15) == 0;
     if (quarter < my_warps) {
-      float o[D];
-      if (tiles > 0) {
-#pragma unroll
-        for (int c = 0; c < D; c += 32) tmem_load(output + c, (uint32_t*)o + c);
-        tmem_loaded();
-      } else {
-#pragma unroll
-        for (int c = 0; c < D; ++c) o[c] = 0.f;
-      }
       if (*(volatile uint32_t*)gave_up) sum = __uint_as_float(0x7FC00000u);  // NaN: seen by whoever reads the output
-      if (p.split > 1) {
-        const int at = s * 128 + row;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const int r = m / p.group, g = m - r * p.group, at = s * 128 + row;
+      __nv_bfloat16* out = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h;
 #pragma unroll
-        for (int c = 0; c < D; c += 4) *(float4*)(parts + at * P::kPartRow + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-        tops[at] = top;
-        sums[at] = sum;
-      } else if (m < m1) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int r = m / p.group, g = m - r * p.group;
-        __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h;
+      for (int c0 = 0; c0 < D; c0 += 32) {
+        uint32_t o[32];
+        if (tiles > 0) {
+          tmem_load(output + c0, o);
+          tmem_loaded();
+        } else {
 #pragma unroll
-        for (int c = 0; c < D; c += 8) {
-          const uint4 y = make_uint4(pair(o[c] * inv, o[c + 1] * inv), pair(o[c + 2] * inv, o[c + 3] * inv),
-                                     pair(o[c + 4] * inv, o[c + 5] * inv), pair(o[c + 6] * inv, o[c + 7] * inv));
-          if (wide) {
-            *(uint4*)(at + c) = y;
-          } else {
-            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+          for (int c = 0; c < 32; ++c) o[c] = 0;
+        }
+        if (p.split > 1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ((unsigned short*)at)[c + j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+          for (int c = 0; c < 32; c += 4) *(uint4*)(parts + at * P::kPartRow + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+        } else if (m < m1) {
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = pair(__uint_as_float(o[c + 2 * j]) * inv, __uint_as_float(o[c + 2 * j + 1]) * inv);
+            if (wide) {
+              *(uint4*)(out + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) ((unsigned short*)out)[c0 + c + j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+            }
           }
         }
       }
+      tops[at] = top;
+      sums[at] = sum;
     }
   }
 
