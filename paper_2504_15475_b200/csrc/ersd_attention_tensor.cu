@@ -6,11 +6,17 @@
 // weights go back there as bfloat16 over scores they came from, and the second product takes them from there.
 // Two builds:
 //   Few<D>   up to 128 packed rows (decoding, drafts), where the cache's bytes bound the call: 64 slots at a time,
-//            scores in two buffers so that the next product of scores runs during a softmax.  Either with half of
-//            an SM's shared and tensor memory, so that two blocks share an SM and one's start and end hide behind
-//            the other, or, for calls of no more blocks than SMs, with a ring three times as long.
+//            scores in two buffers, so that the next product of scores runs during a softmax; a warp each issues the
+//            two products, since what bounds a tile is the waits of the one that issues.  Either with half of an
+//            SM's shared and tensor memory, so that two blocks share an SM and one's start and end hide behind the
+//            other, or, for calls of no more blocks than SMs, with rings three times as long.  The product has
+//            128 rows whether they are there or not: up to 32 rows are put there four times, up to 64 twice, and
+//            each copy's warps take a part of the slots, which divides the softmax's time (a warp's powers of two for
+//            64 slots alone take 512 cycles) by as much; the copies' outputs are joined at the end.
 //   Many<D>  256 packed rows (long chunks), where products and powers of two do: two streams of 128 rows with a
-//            softmax group each, 128 slots at a time; one's products run while the other's softmax does.
+//            softmax group each, 128 slots at a time (with 64 the first operand, read again for every 64 columns,
+//            takes more of shared memory's rate than there is: 2545 cycles for 64 slots against 3660 for 128); one's
+//            products run while the other's softmax does, and half of a tile's weights go ahead of the rest.
 //
 // The output's accumulator stays in tensor memory.  It is scaled only when a row's maximum has risen by more than
 // 2^8 since the last time (weights are then at most 2^8, which bfloat16 and the 32-bit sums hold as well as 1);
@@ -23,6 +29,7 @@
 #include <math.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "ersd_attention.cuh"
 
@@ -36,49 +43,47 @@ constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before 
 
 template <int D_, int kBlocks_>
 struct Few {
-  static constexpr int D = D_, kStreams = 1, kN = 64, kBuffers = 2;
-  static constexpr int kKeyStages = kBlocks_ == 2 ? (D == 64 ? 4 : 2) : (D == 64 ? 8 : 6), kValueStages = kKeyStages;
+  static constexpr int D = D_, kStreams = 1, kN = 64;
+  static constexpr int kStages = kBlocks_ == 2 ? (D == 64 ? 4 : 2) : (D == 64 ? 8 : 6);  // of each ring
   static constexpr int kWarps = 4, kThreads = 256, kBlocks = kBlocks_, kColumns = 256;
 };
 template <int D_>
 struct Many {
-  static constexpr int D = D_, kStreams = 2, kN = 128, kBuffers = 1;
-  static constexpr int kKeyStages = D == 64 ? 6 : 3, kValueStages = D == 64 ? 6 : 2;
+  static constexpr int D = D_, kStreams = 2, kN = 128;
+  static constexpr int kStages = D == 64 ? 5 : 2;
   // (the last four warps are a group that gives its registers to the others)
   static constexpr int kWarps = 8, kThreads = 384, kBlocks = 1, kColumns = 512;
   static constexpr int kRegistersSoftmax = 200, kRegistersOthers = 104;  // 2 * 200 + 104 = 3 * 168, what a launch gives
 };
 
-constexpr int kTableRing = 8;  // tiles whose table entries are on their way or in use
-
 struct Ring {  // of keys or values
   uint64_t full[8], empty[8];
-  int32_t entries[kTableRing][32];
 };
 struct Misc {  // behind the rings
   Ring ring[2];                  // keys, values
-  uint64_t scores[2];            // of a stream (or a buffer) are in tensor memory
-  uint64_t weights[2];           // and the weights that take their place.  (A buffer's own: with one barrier for both
+  uint64_t scores[2];            // of a buffer (of the stream, or of a stream) are in tensor memory
+  uint64_t half[2];              // with 128 slots: the weights of the first 64 are
+  uint64_t weights[2];           // and all weights, which take the scores' place.  (A buffer's own: with one barrier for both
                                  // a quick warp's next tile would count for a slow warp's last.)
-  uint64_t rest[2];              // a stream's output is at rest: the product with the last weights is done
+  uint64_t rest[2];              // Few: the product with a buffer's weights is done
   uint64_t done;                 // all products
   uint64_t q_there;              // q's rows are in shared memory
   uint32_t tmem;
   uint32_t gave_up;              // a wait ran out: nothing that follows it can be trusted
   uint8_t parent[ERSD_MAX_ROWS], depth[ERSD_MAX_ROWS];
 };
-static_assert(sizeof(Misc) <= 3072, "");
+static_assert(sizeof(Misc) <= 2048, "");
 
 template <typename C>
 struct Plan : C {
-  static constexpr int D = C::D, kN = C::kN, kStages = C::kKeyStages + C::kValueStages;
+  static constexpr int D = C::D, kN = C::kN;
   static constexpr int kRows = C::kStreams * 128;
   static constexpr int kStageBytes = kN * D * 2;  // keys or values of a tile
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kSmem = kQBytes + kStages * kStageBytes + 3072;
-  static constexpr int kOutputs = C::kStreams * C::kBuffers * kN;  // first column of the outputs
+  static constexpr int kSmem = kQBytes + 2 * C::kStages * kStageBytes + 2048;
+  static constexpr int kOutputs = 2 * kN;  // first column of the outputs
   static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
-  static_assert(kRows * (kPartRow + 2) * 4 <= kQBytes + kStages * kStageBytes, "");
+  static_assert(kRows * (kPartRow + 2) * 4 <= kQBytes + 2 * C::kStages * kStageBytes, "");
   static_assert(kOutputs + C::kStreams * D <= C::kColumns, "");
   // No more than kBlocks blocks fit on an SM by shared memory, and their tensor memory fits with them: a block
   // never waits for another's tensor memory, which could not be given up by one that waits for it in a cluster.
@@ -178,6 +183,9 @@ __device__ __forceinline__ void tmem_load_16(uint32_t at, uint32_t* r) {
       : R8(r, 0), R8(r, 8)
       : "r"(at));
 }
+__device__ __forceinline__ void tmem_store_8(uint32_t at, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::S8(r, 0), "r"(at) : "memory");
+}
 __device__ __forceinline__ void tmem_store_16(uint32_t at, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::S8(r, 0),
@@ -220,9 +228,6 @@ __device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
   return y;
 }
-__device__ __forceinline__ void copy_entry(int32_t* to, const int32_t* from) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_address(to)), "l"(from) : "memory");
-}
 
 // Bits [a, b) of a word, both cut to 0..32.
 __device__ __forceinline__ uint32_t bits_between(int a, int b) {
@@ -237,14 +242,14 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     attention_tensor_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map,
                             const __grid_constant__ CUtensorMap v_map, const int box) {
   using P = Plan<C>;
-  constexpr int D = P::D, kN = P::kN, kStreams = C::kStreams, kBuffers = C::kBuffers;
+  constexpr int D = P::D, kN = P::kN, kStreams = C::kStreams, kStages = C::kStages;
   constexpr int kPanel = kN * 128, kQPanel = 128 * 128;  // bytes of a panel: rows of 64 elements
   constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = C::kWarps + 2;  // (the last two: warps)
   extern __shared__ __align__(1024) char raw[];
   char* q_tile = raw;
   char* key_ring = q_tile + P::kQBytes;
-  char* value_ring = key_ring + C::kKeyStages * P::kStageBytes;
-  Misc& sh = *(Misc*)(value_ring + C::kValueStages * P::kStageBytes);
+  char* value_ring = key_ring + kStages * P::kStageBytes;
+  Misc& sh = *(Misc*)(value_ring + kStages * P::kStageBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kv_head = blockIdx.y, b = blockIdx.z;
   const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
@@ -256,10 +261,8 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         barrier_init(&sh.ring[s].full[i], 1);
         barrier_init(&sh.ring[s].empty[i], 1);
       }
-    for (int s = 0; s < 2; ++s) {
-      barrier_init(&sh.scores[s], 1);
-      barrier_init(&sh.rest[s], 1);
-    }
+    for (int i = 0; i < 2; ++i) barrier_init(&sh.scores[i], 1);
+    for (int s = 0; s < 2; ++s) barrier_init(&sh.rest[s], 1);
     barrier_init(&sh.done, 1);
     barrier_init(&sh.q_there, C::kWarps);
     sh.gave_up = (smem_address(raw) & 1023) != 0;  // (the operands' layout wants it so)
@@ -291,11 +294,6 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     const unsigned short* e = (const unsigned short*)at;
     return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
   };
-  auto store_q = [&](int i, const uint4& x) {  // in the operand's layout
-    const int m = i / kPieces, c = i % kPieces, row = m & 127;
-    *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kQPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-        make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-  };
   uint4 early[kEarly];
   const int most = (min(m0 + P::kRows, p.R * p.group) - m0) * kPieces;
   if (warp < C::kWarps) {
@@ -309,8 +307,10 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   rows = max(0, min(rows, p.R));
   const int m1 = max(m0, min(m0 + P::kRows, rows * p.group));  // (no rows: the same for every block of the cluster)
   const int r0 = m0 / p.group, r1 = max(r0, (m1 - 1) / p.group + 1);
-  // warps of each stream with rows
-  const int warps0 = (min(m1 - m0, 128) + 31) / 32, warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
+  // how often the rows are there, and the warps of each stream with rows
+  const int copies = kStreams == 2 || m1 - m0 > 64 ? 1 : m1 - m0 > 32 ? 2 : 4, copy_rows = 128 / copies;
+  const int warps0 = copies > 1 && m1 > m0 ? 4 : (min(m1 - m0, 128) + 31) / 32;
+  const int warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
   int min_depth = r0;
   if (p.tree && m1 > m0) {
     min_depth = p.depth[r0];
@@ -321,7 +321,10 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   const int t0 = (int)((int64_t)all_tiles * part / p.split), t1 = (int)((int64_t)all_tiles * (part + 1) / p.split);
   const int tiles = t1 - t0;
   if (tid == 0) {
-    for (int s = 0; s < 2; ++s) barrier_init(&sh.weights[s], (uint32_t)max(1, s && kStreams == 2 ? warps1 : warps0));
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(&sh.half[i], (uint32_t)max(1, kStreams == 1 || i == 0 ? warps0 : warps1));
+      barrier_init(&sh.weights[i], (uint32_t)max(1, kStreams == 1 || i == 0 ? warps0 : warps1));
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   before_sync();
@@ -333,6 +336,22 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   float* parts = (float*)q_tile;                        // [rows][kPartRow]
   float* tops = parts + P::kRows * P::kPartRow;        // [rows]
   float* sums = tops + P::kRows;                       // [rows]
+  const bool joins = copies > 1 || p.split > 1;  // whether outputs go through shared memory
+  // Four columns of a row's joined output.
+  const bool out_wide = ((p.o_b | p.o_r | p.o_h) & 3) == 0 && ((uintptr_t)p.out & 7) == 0;
+  auto write_row = [&](int row, int d, const float4& y, float total) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int r = (m0 + row) / p.group, g = m0 + row - r * p.group;
+    __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h + d;
+    const uint2 x = make_uint2(pair(y.x * inv, y.y * inv), pair(y.z * inv, y.w * inv));
+    if (out_wide) {
+      *(uint2*)at = x;
+    } else {
+      const uint32_t w[2] = {x.x, x.y};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ((unsigned short*)at)[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+    }
+  };
   auto products_done = [&]() {
     // (asked for in every case: after a wait that ran out, products may still be under way)
     if (tiles > 0)
@@ -344,112 +363,156 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   if (warp >= C::kWarps) {
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersOthers));
     if (warp == kCopies || warp == kCopies + 1) {
-      // ---- copies of keys, of values: a lane has a box or two (`box` slots by 64 elements) of every tile.  The entries
-      // of the block table come through shared memory, so that no register waits for them.
+      // ---- copies of keys, of values: a lane has a box (`box` slots by 64 elements) of every tile, or the two of its
+      // slots.  64 entries of the block table are in the warp's registers, the later 32 asked for 32 pages before
+      // they are needed.  All that a tile's copies need is worked out before the wait for their place.
       const bool values = warp != kCopies;
-      const int stages = values ? C::kValueStages : C::kKeyStages;
       const CUtensorMap* map = values ? &v_map : &k_map;
       char* const places = values ? value_ring : key_ring;
       Ring& ring = sh.ring[values];
       const int groups = kN / box, boxes = groups * (D / 64), shift = __ffs(groups) - 1;
-      const int group = lane & (groups - 1), panel = lane >> shift;  // of the lane's first box; a second one is 32 boxes on
+      const int group = lane & (groups - 1), panel = lane >> shift;
       const int32_t* table = p.table + b * p.table_stride;
-      auto needs = [&](int slot) { return slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo); };
-      auto ask = [&](int t) {
-        if (t < tiles && lane < groups) {
-          const int slot = tile_start<kN>(keys, t0 + t) + lane * box;
-          if (needs(slot)) copy_entry(&ring.entries[t % kTableRing][lane], table + page_of(p, slot));
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+      const int last_entry = page_of(p, p.capacity - 1);
+      auto entry = [&](int i) { return table[min(i, last_entry)]; };
+      int first_entry = 0;
+      int32_t near = 0, far = 0;  // entries first_entry + lane, and 32 on
+      auto refill = [&](int from) {
+        first_entry = from;
+        near = entry(from + lane);
+        far = entry(from + 32 + lane);
       };
-      constexpr int kAhead = kTableRing - 1;
-#pragma unroll
-      for (int t = 0; t < kAhead; ++t) ask(t);
+      if (tiles > 0) refill(page_of(p, tile_start<kN>(keys, t0)));
       int stage = 0, t = 0;
       uint32_t parity = 1;  // of the ring's round before: nothing to wait for in the first
       for (; t < tiles; ++t) {
-        const int start = tile_start<kN>(keys, t0 + t);
+        const int start = tile_start<kN>(keys, t0 + t), end_entry = page_of(p, min(start + kN, p.capacity) - 1);
+        if (end_entry >= first_entry + 64) {
+          if (page_of(p, start) >= first_entry + 32 && end_entry < first_entry + 96) {
+            first_entry += 32;
+            near = far;
+            far = entry(first_entry + 32 + lane);
+          } else {  // behind a gap between first tokens and window (64 entries hold any tile: pages are of four slots and more)
+            refill(page_of(p, start));
+          }
+        }
+        const int slot = start + group * box, at = page_of(p, min(slot, p.capacity - 1));
+        const int32_t page_near = __shfl_sync(0xFFFFFFFFu, near, at - first_entry & 31), page_far = __shfl_sync(0xFFFFFFFFu, far, at - first_entry & 31);
+        int page = at - first_entry < 32 ? page_near : page_far;
+        if (page < 0 || page >= p.num_pages) page = p.num_pages;  // (outside the cache: such a page gives zeros)
+        const int token = slot - at * p.page_size;
+        const bool needed = lane < boxes && slot < keys.hi && !(slot >= keys.sink_hi && slot + box <= keys.lo);
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, needed)) * (uint32_t)box * (boxes > 32 ? 256u : 128u);
         uint64_t* full = &ring.full[stage];
-        ask(t + kAhead);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-        if (t >= stages && !barrier_wait(&ring.empty[stage], parity, gave_up)) break;
-        const uint32_t count = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, lane < groups && needs(start + lane * box))) * (D / 64);
-        if (lane == 0) barrier_expect(full, count * (uint32_t)box * 128u);
+        const uint32_t to = smem_address(places + stage * P::kStageBytes) + group * box * 128;
+        if (t >= kStages && !barrier_wait(&ring.empty[stage], parity, gave_up)) break;
+        if (lane == 0) barrier_expect(full, bytes);
         __syncwarp();
-        const uint32_t to = smem_address(places + stage * P::kStageBytes);
-        for (int i = lane, g = group, c = panel; i < boxes; i += 32, g = i & (groups - 1), c = i >> shift) {
-          const int slot = start + g * box;
-          if (!needs(slot)) continue;
-          const int page = ring.entries[t % kTableRing][g];  // (outside the cache: such a page gives zeros)
-          tma_box(to + c * kPanel + g * box * 128, map, c * 64, slot - page_of(p, slot) * p.page_size, kv_head,
-                  page < 0 || page >= p.num_pages ? p.num_pages : page, full);
+        if (needed) {
+          tma_box(to + panel * kPanel, map, panel * 64, token, kv_head, page, full);
+          if (boxes > 32) tma_box(to + kPanel, map, 64, token, kv_head, page, full);
         }
         __syncwarp();
-        if (++stage == stages) {
+        if (++stage == kStages) {
           stage = 0;
           parity ^= 1;
         }
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
       // every copy has landed before the block ends, even where the products gave up
       if (*(volatile uint32_t*)gave_up)
-        for (int x = max(0, t - stages); x < t; ++x)
-          for (int i = 0; i < (1 << 22) && !barrier_try(&ring.full[x % stages], (uint32_t)(x / stages) & 1); ++i) {
+        for (int x = max(0, t - kStages); x < t; ++x)
+          for (int i = 0; i < (1 << 22) && !barrier_try(&ring.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
           }
       __syncwarp();
-    } else if (warp == kProducts) {
-      // ---- products: the warp stays together, one thread issues
-      if (tiles > 0) {
-        constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
-        const int streams = kStreams == 2 && warps1 > 0 ? 2 : 1;
-        const bool leader = elected();
-        const uint64_t q_operand = operand(smem_address(q_tile), 16), key_operand = operand(smem_address(key_ring), 16),
-                       value_operand = operand(smem_address(value_ring), kPanel);
-        int key_stage = 0, value_stage = 0;
-        uint32_t key_parity = 0, value_parity = 0;
-        // Scores of stream s with tile t.  (Addresses are in steps of 16 bytes in an operand's lowest bits.)
-        auto score = [&](int s, int t) {
-          const int buffer = kBuffers == 2 ? t & 1 : s;
-          if (s == 0 && !barrier_wait(&sh.ring[0].full[key_stage], key_parity, gave_up)) return false;
-          after_sync();
-          const uint64_t a = q_operand + (uint32_t)(s * (128 * D * 2 >> 4)), k = key_operand + (uint32_t)(key_stage * (P::kStageBytes >> 4));
-          if (leader) {
+    } else if (warp == kProducts || (kStreams == 1 && warp == kProducts + 1)) {
+      // ---- products: a warp stays together, one thread issues.  Few: a warp for the scores, a warp for the outputs.
+      // Many: one warp for both, since a stream's scores take the place of the weights that the product before uses.
+      constexpr uint32_t kScores = instruction(kN, false), kOutput = instruction(D, true);
+      const int streams = kStreams == 2 && warps1 > 0 ? 2 : 1;
+      const bool leader = elected();
+      const uint64_t q_operand = operand(smem_address(q_tile), 16), key_operand = operand(smem_address(key_ring), 16),
+                     value_operand = operand(smem_address(value_ring), kPanel);
+      int key_stage = 0, value_stage = 0;
+      uint32_t key_parity = 0, value_parity = 0;
+      // Scores of stream s into `buffer`.  (Addresses are in steps of 16 bytes in an operand's lowest bits.)
+      auto score = [&](int s, int buffer) {
+        if (s == 0 && !barrier_wait(&sh.ring[0].full[key_stage], key_parity, gave_up)) return false;
+        after_sync();
+        const uint64_t a = q_operand + (uint32_t)(s * (128 * D * 2 >> 4)), k = key_operand + (uint32_t)(key_stage * (P::kStageBytes >> 4));
+        if (leader) {
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j)
-              mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4),
-                         k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4), kScores, j > 0);
-            mma_commit(&sh.scores[buffer]);
-            if (s == streams - 1) mma_commit(&sh.ring[0].empty[key_stage]);
+          for (int j = 0; j < D / 16; ++j)
+            mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4),
+                       k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4), kScores, j > 0);
+          mma_commit(&sh.scores[buffer]);
+          if (s == streams - 1) mma_commit(&sh.ring[0].empty[key_stage]);
+        }
+        __syncwarp();
+        if (s == streams - 1 && ++key_stage == kStages) {
+          key_stage = 0;
+          key_parity ^= 1;
+        }
+        return true;
+      };
+      // The output of stream s from four of the tile's steps of 16 slots, from step `from` on.
+      auto output = [&](int s, int t, int buffer, int from) {
+        after_sync();
+        const uint64_t v = value_operand + (uint32_t)(value_stage * (P::kStageBytes >> 4));
+        if (leader) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + (from + j) * 8, v + (uint32_t)((from + j) * 16 * 128 >> 4), kOutput,
+                     t > 0 || from + j > 0);
+        }
+        __syncwarp();
+      };
+      bool ok = true;
+      if constexpr (kStreams == 1) {
+        if (warp == kProducts) {
+          ok = barrier_wait(&sh.q_there, 0, gave_up);
+          for (int t = 0; ok && t < tiles; ++t) {
+            // (the weights that were in this buffer are used up)
+            if (t >= 2) ok = barrier_wait(&sh.rest[t & 1], (uint32_t)(t / 2 - 1) & 1, gave_up);
+            ok = ok && score(0, t & 1);
           }
-          __syncwarp();
-          if (s == streams - 1 && ++key_stage == C::kKeyStages) {
-            key_stage = 0;
-            key_parity ^= 1;
-          }
-          return true;
-        };
-        bool ok = barrier_wait(&sh.q_there, 0, gave_up);
-        for (int t = 0; ok && t < kBuffers && t < tiles; ++t)
-          for (int s = 0; ok && s < streams; ++s) ok = score(s, t);
-        for (int t = 0; ok && t < tiles; ++t) {
-          for (int s = 0; ok && s < streams; ++s) {
-            const int buffer = kBuffers == 2 ? t & 1 : s;
-            if (s == 0) ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up);
-            ok = ok && barrier_wait(&sh.weights[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up);
+        } else if (tiles > 0) {
+          for (int t = 0; t < tiles; ++t) {
+            ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up) &&
+                 barrier_wait(&sh.weights[t & 1], (uint32_t)(t >> 1) & 1, gave_up);
             if (!ok) break;
-            after_sync();
-            const uint64_t v = value_operand + (uint32_t)(value_stage * (P::kStageBytes >> 4));
+            output(0, t, t & 1, 0);
             if (leader) {
-#pragma unroll
-              for (int j = 0; j < kN / 16; ++j)
-                mma_tmem(tmem + P::kOutputs + s * D, tmem + buffer * kN + j * 8, v + (uint32_t)(j * 16 * 128 >> 4), kOutput, t > 0 || j > 0);
-              if (kBuffers == 2) mma_commit(&sh.rest[s]);
-              if (s == streams - 1) mma_commit(&sh.ring[1].empty[value_stage]);
+              mma_commit(&sh.rest[t & 1]);
+              mma_commit(&sh.ring[1].empty[value_stage]);
             }
             __syncwarp();
-            if (t + kBuffers < tiles) ok = score(s, t + kBuffers);
+            if (++value_stage == kStages) {
+              value_stage = 0;
+              value_parity ^= 1;
+            }
           }
-          if (++value_stage == C::kValueStages) {
+          if (leader) mma_commit(&sh.done);
+          __syncwarp();
+        }
+      } else if (tiles > 0) {
+        ok = barrier_wait(&sh.q_there, 0, gave_up);
+        for (int s = 0; ok && s < streams; ++s) ok = score(s, s);
+        for (int t = 0; ok && t < tiles; ++t) {
+          for (int s = 0; ok && s < streams; ++s) {
+            if (s == 0) ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up);
+            ok = ok && barrier_wait(&sh.half[s], (uint32_t)t & 1, gave_up);
+            if (!ok) break;
+            output(s, t, s, 0);
+            ok = barrier_wait(&sh.weights[s], (uint32_t)t & 1, gave_up);
+            if (!ok) break;
+            output(s, t, s, 4);
+            if (s == streams - 1) {
+              if (leader) mma_commit(&sh.ring[1].empty[value_stage]);
+              __syncwarp();
+            }
+            if (t + 1 < tiles) ok = score(s, s);
+          }
+          if (++value_stage == kStages) {
             value_stage = 0;
             value_parity ^= 1;
           }
@@ -464,6 +527,12 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersSoftmax));
     {  // rows of q that are not there stay as they are: their scores go nowhere
       const int pieces = (m1 - m0) * kPieces;
+      auto store_q = [&](int i, const uint4& x) {  // in the operand's layout
+        const int m = i / kPieces, c = i % kPieces;
+        for (int row = m & 127; row < 128; row += copy_rows)
+          *(uint4*)(q_tile + (m >> 7) * (128 * D * 2) + (c >> 3) * kQPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+              make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+      };
 #pragma unroll
       for (int j = 0; j < kEarly; ++j)
         if (tid + j * kSoftmaxThreads < pieces) store_q(tid + j * kSoftmaxThreads, early[j]);
@@ -472,14 +541,16 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       __syncwarp();
       if (lane == 0) barrier_arrive(&sh.q_there);
     }
-    const int s = warp >> 2, quarter = warp & 3;
-    const int row = quarter * 32 + lane, m = m0 + s * 128 + row;
-    const int my_warps = s ? warps1 : warps0;
+    const int s = warp >> 2, quarter = warp & 3, my_warps = s ? warps1 : warps0;
+    const int place = quarter * 32 + lane, copy = place / copy_rows, m = m0 + s * 128 + place % copy_rows;
     float top = -INFINITY, sum = 0.f;  // the maximum that the row's weights were formed with, their sum
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, output = tmem + lanes + P::kOutputs + s * D;
-    if (quarter < my_warps) {
+
+    // The tiles of keys, W = 64 / copies slots of each.
+    auto all_tiles_of = [&](auto width) {
+      constexpr int W = decltype(width)::value;
       const float scale = fabsf(p.scale_log2);
-      const int r = min(m, m1 - 1) / p.group;  // (rows of a warp behind the last: as the last, and not written)
+      const int r = min(m, m1 - 1) / p.group;  // (rows behind the last: as the last, and not written)
       const int depth = p.tree ? (int)sh.depth[r] : r;
       const int lo = p.window ? max(0, ctx + depth - p.window + 1) : 0;   // cached slots from lo on, and below `sinks`
       const int hi = min(keys.hi, p.tree ? ctx : ctx + r + 1);
@@ -489,46 +560,50 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       const int all_hi = min(keys.hi, p.tree ? ctx : ctx + first_m / p.group + 1);
       const int all_lo = p.window ? ctx + (p.tree ? p.R - 1 : last_m / p.group) - p.window + 1 : 0;
       for (int t = 0; t < tiles; ++t) {
-        const int start = tile_start<kN>(keys, t0 + t), buffer = kBuffers == 2 ? t & 1 : s;
+        const int tile_at = tile_start<kN>(keys, t0 + t), start = tile_at + copy * W, buffer = kStreams == 1 ? t & 1 : s;
         const uint32_t scores = tmem + lanes + buffer * kN;
-        if (!barrier_wait(&sh.scores[buffer], (uint32_t)(kBuffers == 2 ? t >> 1 : t) & 1, gave_up)) break;
+        if (!barrier_wait(&sh.scores[buffer], (uint32_t)(kStreams == 1 ? t >> 1 : t) & 1, gave_up)) break;
         after_sync();
-        uint32_t x[kN];
+        uint32_t x[W];
+        if constexpr (W == 16) {
+          tmem_load_16(scores + copy * W, x);
+        } else {
 #pragma unroll
-        for (int c = 0; c < kN; c += 32) tmem_load(scores + c, x + c);
+          for (int c = 0; c < W; c += 32) tmem_load(scores + copy * W + c, x + c);
+        }
         tmem_loaded();
-        const bool whole = start + kN <= all_hi && (start >= all_lo || start + kN <= p.sinks);
+        const bool whole = tile_at + kN <= all_hi && (tile_at >= all_lo || tile_at + kN <= p.sinks);
         if (!whole) {
-          uint32_t see[kN / 32];
+          uint32_t see[(W + 31) / 32];
 #pragma unroll
-          for (int w = 0; w < kN / 32; ++w) {
+          for (int w = 0; w < (W + 31) / 32; ++w) {
             const int at = start + 32 * w;
             see[w] = bits_between(lo - at, hi - at) | bits_between(-at, sinks - at);
           }
           if (p.tree) {
             for (int n = r;; n = sh.parent[n]) {
               const int pos = ctx + (int)sh.depth[n], at = ctx + n - start;
-              if (at >= 0 && at < kN && ctx + n < keys.hi && (!p.window || pos >= lo || pos < p.sinks)) {
+              if (at >= 0 && at < W && ctx + n < keys.hi && (!p.window || pos >= lo || pos < p.sinks)) {
                 const uint32_t bit = 1u << (at & 31);
 #pragma unroll
-                for (int w = 0; w < kN / 32; ++w) see[w] |= (at >> 5) == w ? bit : 0u;
+                for (int w = 0; w < (W + 31) / 32; ++w) see[w] |= (at >> 5) == w ? bit : 0u;
               }
               if (n == 0) break;
             }
             __syncwarp();
           }
 #pragma unroll
-          for (int c = 0; c < kN; ++c) x[c] = see[c >> 5] >> (c & 31) & 1u ? x[c] : 0xFF800000u;
+          for (int c = 0; c < W; ++c) x[c] = see[c >> 5] >> (c & 31) & 1u ? x[c] : 0xFF800000u;
           // Values of slots that no row of the block sees are whatever was there: 0 * NaN is no 0.  (Both streams
           // may write the same zeros.)
-          bool any_dead = keys.dead(start) || keys.dead(start + kN - 1);
-          if (!any_dead) any_dead = keys.sink_hi < keys.lo && keys.sink_hi < start + kN && keys.lo > start;
+          bool any_dead = keys.dead(tile_at) || keys.dead(tile_at + kN - 1);
+          if (!any_dead) any_dead = keys.sink_hi < keys.lo && keys.sink_hi < tile_at + kN && keys.lo > tile_at;
           if (any_dead) {
-            if (!barrier_wait(&sh.ring[1].full[t % C::kValueStages], (uint32_t)(t / C::kValueStages) & 1, gave_up)) break;
+            if (!barrier_wait(&sh.ring[1].full[t % kStages], (uint32_t)(t / kStages) & 1, gave_up)) break;
             // the stream's warps share the tile's rows
-            for (int n = row; n < kN; n += my_warps * 32)
-              if (keys.dead(start + n)) {
-                char* v = value_ring + (t % C::kValueStages) * P::kStageBytes + n * 128;
+            for (int n = place; n < kN; n += my_warps * 32)
+              if (keys.dead(tile_at + n)) {
+                char* v = value_ring + (t % kStages) * P::kStageBytes + n * 128;
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c)
 #pragma unroll
@@ -540,7 +615,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         }
         float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < kN; c += 8)
+        for (int c = 0; c < W; c += 8)
 #pragma unroll
           for (int j = 0; j < 4; ++j) a[j] = max3(a[j], __uint_as_float(x[c + 2 * j]), __uint_as_float(x[c + 2 * j + 1]));
         const float now = max3(fmaxf(a[0], a[1]), a[2], a[3]) * scale;
@@ -548,10 +623,10 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         if (t == 0) {
           top = now;
         } else if (__any_sync(0xFFFFFFFFu, rise)) {
-          // The output has to be at rest.  (With one buffer it is: this tile's scores come after the product with the
-          // last weights.)
-          if (kBuffers == 2) {
-            if (!barrier_wait(&sh.rest[s], (uint32_t)(t - 1) & 1, gave_up)) break;
+          // The output has to be at rest.  (In Many it is: this tile's scores come after the product with the last
+          // weights.)
+          if (kStreams == 1) {
+            if (!barrier_wait(&sh.rest[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1, gave_up)) break;
             after_sync();
           }
           const float f = rise ? power_of_two(top - now) : 1.0f;
@@ -570,11 +645,12 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         const float minus = top == -INFINITY ? 0.f : -top;
         const uint64_t scale_two = two(scale, scale), minus_two = two(minus, minus);
         uint64_t both[2] = {0, 0};
+        constexpr int kStep = W == 16 ? 16 : 32;
 #pragma unroll
-        for (int c0 = 0; c0 < kN; c0 += 32) {
-          uint32_t w[16];
+        for (int c0 = 0; c0 < W; c0 += kStep) {
+          uint32_t w[kStep / 2];
 #pragma unroll
-          for (int c = 0; c < 32; c += 2) {
+          for (int c = 0; c < kStep; c += 2) {
             float e0, e1;
             apart(fma_two(two(__uint_as_float(x[c0 + c]), __uint_as_float(x[c0 + c + 1])), scale_two, minus_two), e0, e1);
             e0 = power_of_two(e0);
@@ -582,7 +658,24 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
             both[c >> 1 & 1] = add_two(both[c >> 1 & 1], two(e0, e1));
             w[c >> 1] = pair(e0, e1);
           }
-          tmem_store_16(scores + c0 / 2, w);
+          if constexpr (W == 16) tmem_store_8(scores + copy * W / 2, w);
+          else tmem_store_16(scores + (copy * W + c0) / 2, w);
+          if (kN == 128 && c0 == 32) {
+            tmem_stored();
+            before_sync();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(&sh.half[s]);
+          }
+        }
+        // the other copies' slots have no weight in this one
+        if (W < kN) {
+          const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+          for (int c0 = 0; c0 < kN; c0 += kStep)
+            if (c0 / W != copy) {
+              if constexpr (W == 16) tmem_store_8(scores + c0 / 2, none);
+              else tmem_store_16(scores + c0 / 2, none);
+            }
         }
         float s0, s1;
         apart(add_two(both[0], both[1]), s0, s1);
@@ -592,6 +685,15 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         __syncwarp();
         if (lane == 0) barrier_arrive(&sh.weights[buffer]);
       }
+    };
+    if (quarter < my_warps) {
+      if constexpr (kStreams == 1) {
+        if (copies == 4) all_tiles_of(std::integral_constant<int, 16>());
+        else if (copies == 2) all_tiles_of(std::integral_constant<int, 32>());
+        else all_tiles_of(std::integral_constant<int, 64>());
+      } else {
+        all_tiles_of(std::integral_constant<int, kN>());
+      }
     }
     // ---- the end: every product is done, q's rows and the ring are free
     products_done();
@@ -599,7 +701,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     if (quarter < my_warps) {
       if (*(volatile uint32_t*)gave_up) sum = __uint_as_float(0x7FC00000u);  // NaN: seen by whoever reads the output
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      const int r = m / p.group, g = m - r * p.group, at = s * 128 + row;
+      const int r = m / p.group, g = m - r * p.group, at = s * 128 + place;
       __nv_bfloat16* out = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h;
 #pragma unroll
       for (int c0 = 0; c0 < D; c0 += 32) {
@@ -611,7 +713,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
 #pragma unroll
           for (int c = 0; c < 32; ++c) o[c] = 0;
         }
-        if (p.split > 1) {
+        if (joins) {
 #pragma unroll
           for (int c = 0; c < 32; c += 4) *(uint4*)(parts + at * P::kPartRow + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
         } else if (m < m1) {
@@ -629,11 +731,47 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           }
         }
       }
-      tops[at] = top;
-      sums[at] = sum;
+      if (joins) {
+        tops[at] = top;
+        sums[at] = sum;
+      }
     }
   }
 
+  // ---- the copies' outputs into the first copy's place: out = sum_c 2^(top_c - top) o_c, and so the sums
+  if (copies > 1) {
+    __syncthreads();
+    for (int i = tid; i < (m1 - m0) * (D / 4); i += C::kThreads) {  // (D / 4 divides 32: a row's threads are in one warp)
+      const int row = i / (D / 4), d = (i % (D / 4)) * 4;
+      float most = -INFINITY, total = 0.f;
+      for (int c = 0; c < copies; ++c) most = fmaxf(most, tops[row + c * copy_rows]);
+      const float from = most == -INFINITY ? 0.f : most;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (c >= copies) break;
+        const float theirs = sums[row + c * copy_rows];
+        if (theirs == 0.f) continue;  // saw nothing
+        const float f = power_of_two(tops[row + c * copy_rows] - from);
+        const float4 x = *(const float4*)(parts + (row + c * copy_rows) * P::kPartRow + d);
+        total = fmaf(f, theirs, total);
+        y.x = fmaf(f, x.x, y.x);
+        y.y = fmaf(f, x.y, y.y);
+        y.z = fmaf(f, x.z, y.z);
+        y.w = fmaf(f, x.w, y.w);
+      }
+      if (p.split > 1) {
+        __syncwarp(D == 128 ? 0xFFFFFFFFu : lane < 16 ? 0xFFFFu : 0xFFFF0000u);  // (all have read the row's tops and sums)
+        *(float4*)(parts + row * P::kPartRow + d) = y;
+        if (d == 0) {
+          tops[row] = most;
+          sums[row] = total;
+        }
+      } else {
+        write_row(row, d, y, total);
+      }
+    }
+  }
   if (p.split > 1) {
     cg::cluster_group cluster = cg::this_cluster();
     __syncwarp();
@@ -642,7 +780,6 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     // over the cluster's warps; lane c works out block c's factor, then a lane joins four columns (or, where a head
     // has 64, half a warp a row's half of the blocks).
     constexpr int kD4 = D / 4, kGroups = 32 / kD4;
-    const bool wide = ((p.o_b | p.o_r | p.o_h) & 3) == 0 && ((uintptr_t)p.out & 7) == 0;
     for (int row = warp * p.split + part; row < m1 - m0; row += (C::kThreads / 32) * p.split) {
       float their_top = -INFINITY, their_sum = 0.f;
       if (lane < p.split) {
@@ -678,18 +815,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         y.z += __shfl_xor_sync(0xFFFFFFFFu, y.z, 16);
         y.w += __shfl_xor_sync(0xFFFFFFFFu, y.w, 16);
       }
-      if (first) continue;
-      const float inv = total == 0.f ? 0.f : 1.f / total;
-      const int r = (m0 + row) / p.group, g = m0 + row - r * p.group;
-      __nv_bfloat16* at = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h + d;
-      const uint2 x = make_uint2(pair(y.x * inv, y.y * inv), pair(y.z * inv, y.w * inv));
-      if (wide) {
-        *(uint2*)at = x;
-      } else {
-        const uint32_t w[2] = {x.x, x.y};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ((unsigned short*)at)[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
-      }
+      if (first == 0) write_row(row, d, y, total);
     }
     __syncwarp();
     cluster.sync();  // (no block ends while another reads its shared memory)
@@ -736,11 +862,11 @@ bool encode(CUtensorMap* map, const void* at, int D, const AttentionParams& p, i
 
 struct TensorBuild {
   const void* kernel;
-  int smem, rows, threads, blocks, slots;
+  int smem, rows, threads, slots;
 };
 template <typename C>
 TensorBuild tensor_build() {
-  return {(const void*)attention_tensor_kernel<C>, Plan<C>::kSmem, Plan<C>::kRows, C::kThreads, C::kBlocks, C::kN};
+  return {(const void*)attention_tensor_kernel<C>, Plan<C>::kSmem, Plan<C>::kRows, C::kThreads, C::kN};
 }
 
 // What a build needs before its first launch on a device; clusters[i]: how many clusters of 2^i blocks, i <= 4, the
