@@ -388,7 +388,7 @@ typedef struct ersd_chunk_opts {
   int32_t window;            /* attention: 0, or a key is visible only if its position is > the row's - window ... */
   int32_t sinks;             /* ... or < sinks */
   int32_t max_context;       /* attention: 0, or an upper bound of context_lens: only speeds the call up */
-  int32_t split;             /* attention: thread blocks that share a tile of rows, 1, 2, 4, 8, 16; 0 = chosen by the library */
+  int32_t split;             /* attention: thread blocks that share a tile of rows, up to 16; 0 = chosen by the library */
   uint32_t kernel_path;      /* attention: 0 = chosen by the library, 1 = the kernel of 32-bit arithmetic, 2 = the kernel of
                                 tensor-core products (ERSD_EUNSUPPORTED where it does not apply: see below) */
   uint32_t reserved;

@@ -5,14 +5,16 @@
 // (tcgen05.mma), and groups of four warps do the softmax, a thread to a row: scores come out of tensor memory,
 // weights go back there as bfloat16 over scores they came from, and the second product takes them from there.
 // Two builds:
-//   Few<D>   up to 128 packed rows (decoding, drafts), where the cache's bytes bound the call: 64 slots at a time,
-//            scores in two buffers, so that the next product of scores runs during a softmax; a warp each issues the
-//            two products, since what bounds a tile is the waits of the one that issues.  Either with half of an
-//            SM's shared and tensor memory, so that two blocks share an SM and one's start and end hide behind the
-//            other, or, for calls of no more blocks than SMs, with rings three times as long.  The product has
-//            128 rows whether they are there or not: up to 32 rows are put there four times, up to 64 twice, and
-//            each copy's warps take a part of the slots, which divides the softmax's time (a warp's powers of two for
-//            64 slots alone take 512 cycles) by as much; the copies' outputs are joined at the end.
+//   Few<D>   up to 128 packed rows (decoding, drafts), where the cache's bytes bound the call; scores have two or three
+//            buffers, so that the next products of scores run during a softmax, and a warp each issues the two
+//            products, since what bounds a tile is the waits of the one that issues.  Either 64 slots at a time
+//            with half of an SM's shared and tensor memory, so that two blocks share an SM and one's start and end
+//            hide behind the other; or, for calls of no more blocks than SMs, 128 slots at a time with longer rings,
+//            four warps that copy and q in tensor memory (from shared memory it takes 96 cycles for every 64 columns,
+//            from there 32).  The product has 128 rows whether they are there or not: up to 32 rows are put there
+//            four times, up to 64 twice, and each copy's warps take a part of the slots, which divides the softmax's
+//            time (a warp's powers of two for 64 slots alone take 512 cycles) by as much; the copies' outputs are
+//            joined at the end.
 //   Many<D>  256 packed rows (long chunks), where products and powers of two do: two streams of 128 rows with a
 //            softmax group each, 128 slots at a time (with 64 the first operand, read again for every 64 columns,
 //            takes more of shared memory's rate than there is: 2545 cycles for 64 slots against 3660 for 128); one's
@@ -43,16 +45,18 @@ constexpr float kRise = 8.0f;         // a row's maximum may rise by 2^8 before 
 
 template <int D_, int kBlocks_>
 struct Few {
-  static constexpr int D = D_, kStreams = 1, kN = 64;
-  static constexpr int kStages = kBlocks_ == 2 ? (D == 64 ? 4 : 2) : (D == 64 ? 8 : 6);  // of each ring
-  static constexpr int kWarps = 4, kThreads = 256, kBlocks = kBlocks_, kColumns = 256;
+  static constexpr int D = D_, kStreams = 1, kN = kBlocks_ == 1 ? 128 : 64, kBuffers = kBlocks_ == 2 && D == 64 ? 3 : 2;
+  static constexpr int kStages = kBlocks_ == 2 ? (D == 64 ? 4 : 2) : (D == 64 ? 7 : 3);  // of each ring
+  static constexpr bool kQInTmem = kBlocks_ == 1;
+  static constexpr int kWarps = 4, kCopyWarps = kBlocks_ == 1 ? 4 : 2, kThreads = 192 + 32 * kCopyWarps, kBlocks = kBlocks_, kColumns = 512 / kBlocks_;
 };
 template <int D_>
 struct Many {
-  static constexpr int D = D_, kStreams = 2, kN = 128;
+  static constexpr int D = D_, kStreams = 2, kN = 128, kBuffers = 2;  // (a stream has one)
   static constexpr int kStages = D == 64 ? 5 : 2;
+  static constexpr bool kQInTmem = false;
   // (the last four warps are a group that gives its registers to the others)
-  static constexpr int kWarps = 8, kThreads = 384, kBlocks = 1, kColumns = 512;
+  static constexpr int kWarps = 8, kCopyWarps = 2, kThreads = 384, kBlocks = 1, kColumns = 512;
   static constexpr int kRegistersSoftmax = 200, kRegistersOthers = 104;  // 2 * 200 + 104 = 3 * 168, what a launch gives
 };
 
@@ -61,11 +65,11 @@ struct Ring {  // of keys or values
 };
 struct Misc {  // behind the rings
   Ring ring[2];                  // keys, values
-  uint64_t scores[2];            // of a buffer (of the stream, or of a stream) are in tensor memory
+  uint64_t scores[4];            // of a buffer (of the stream, or of a stream) are in tensor memory
   uint64_t half[2];              // with 128 slots: the weights of the first 64 are
-  uint64_t weights[2];           // and all weights, which take the scores' place.  (A buffer's own: with one barrier for both
+  uint64_t weights[4];           // and all weights, which take the scores' place.  (A buffer's own: with one barrier for both
                                  // a quick warp's next tile would count for a slow warp's last.)
-  uint64_t rest[2];              // Few: the product with a buffer's weights is done
+  uint64_t rest[4];              // Few: the product with a buffer's weights is done
   uint64_t done;                 // all products
   uint64_t q_there;              // q's rows are in shared memory
   uint32_t tmem;
@@ -79,12 +83,13 @@ struct Plan : C {
   static constexpr int D = C::D, kN = C::kN;
   static constexpr int kRows = C::kStreams * 128;
   static constexpr int kStageBytes = kN * D * 2;  // keys or values of a tile
-  static constexpr int kQBytes = kRows * D * 2;
+  static constexpr int kQBytes = C::kQInTmem ? 0 : kRows * D * 2;
   static constexpr int kSmem = kQBytes + 2 * C::kStages * kStageBytes + 2048;
-  static constexpr int kOutputs = 2 * kN;  // first column of the outputs
+  static constexpr int kOutputs = C::kBuffers * kN;  // first column of the outputs
+  static constexpr int kQColumn = kOutputs + C::kStreams * D;
   static constexpr int kPartRow = D + 4;  // floats of a row of partial output: 16 bytes on, so that rows fall on other banks
   static_assert(kRows * (kPartRow + 2) * 4 <= kQBytes + 2 * C::kStages * kStageBytes, "");
-  static_assert(kOutputs + C::kStreams * D <= C::kColumns, "");
+  static_assert(kQColumn + (C::kQInTmem ? D / 2 : 0) <= C::kColumns, "");
   // No more than kBlocks blocks fit on an SM by shared memory, and their tensor memory fits with them: a block
   // never waits for another's tensor memory, which could not be given up by one that waits for it in a cluster.
   static_assert((kSmem + 1024) * C::kBlocks <= 228 * 1024 && (kSmem + 1024) * (C::kBlocks + 1) > 228 * 1024, "");
@@ -183,6 +188,13 @@ __device__ __forceinline__ void tmem_load_16(uint32_t at, uint32_t* r) {
       : R8(r, 0), R8(r, 8)
       : "r"(at));
 }
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::S8(r, 0),
+      S8(r, 8), S8(r, 16), S8(r, 24), "r"(at)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_store_8(uint32_t at, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::S8(r, 0), "r"(at) : "memory");
 }
@@ -242,9 +254,9 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
     attention_tensor_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map,
                             const __grid_constant__ CUtensorMap v_map, const int box) {
   using P = Plan<C>;
-  constexpr int D = P::D, kN = P::kN, kStreams = C::kStreams, kStages = C::kStages;
+  constexpr int D = P::D, kN = P::kN, kStreams = C::kStreams, kBuffers = C::kBuffers, kStages = C::kStages;
   constexpr int kPanel = kN * 128, kQPanel = 128 * 128;  // bytes of a panel: rows of 64 elements
-  constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = C::kWarps + 2;  // (the last two: warps)
+  constexpr int kSoftmaxThreads = C::kWarps * 32, kCopies = C::kWarps, kProducts = kCopies + C::kCopyWarps;  // (the last two: warps)
   extern __shared__ __align__(1024) char raw[];
   char* q_tile = raw;
   char* key_ring = q_tile + P::kQBytes;
@@ -261,8 +273,10 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         barrier_init(&sh.ring[s].full[i], 1);
         barrier_init(&sh.ring[s].empty[i], 1);
       }
-    for (int i = 0; i < 2; ++i) barrier_init(&sh.scores[i], 1);
-    for (int s = 0; s < 2; ++s) barrier_init(&sh.rest[s], 1);
+    for (int i = 0; i < kBuffers; ++i) {
+      barrier_init(&sh.scores[i], 1);
+      barrier_init(&sh.rest[i], 1);
+    }
     barrier_init(&sh.done, 1);
     barrier_init(&sh.q_there, C::kWarps);
     sh.gave_up = (smem_address(raw) & 1023) != 0;  // (the operands' layout wants it so)
@@ -286,20 +300,33 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   const __nv_bfloat16* q = (const __nv_bfloat16*)p.q + b * p.q_b;
   const bool q_wide = ((p.q_b | p.q_r | p.q_h) & 7) == 0 && ((uintptr_t)p.q & 15) == 0;
   const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;  // (the softmax takes a positive scale)
-  constexpr int kPieces = D / 8, kEarly = 4;  // of a row, of 16 bytes; asked for early by a thread
-  auto load_q = [&](int i) {
-    const int m = i / kPieces, c = i % kPieces, r = (m0 + m) / p.group, g = m0 + m - r * p.group;
-    const __nv_bfloat16* at = q + r * p.q_r + (kv_head * p.group + g) * p.q_h + c * 8;
+  constexpr int kPieces = D / 8;  // of a row, of 16 bytes
+  auto q_row = [&](int m) {
+    const int r = (m0 + m) / p.group;
+    return q + r * p.q_r + (kv_head * p.group + m0 + m - r * p.group) * p.q_h;
+  };
+  auto load_piece = [&](const __nv_bfloat16* at) {
     if (q_wide) return *(const uint4*)at;
     const unsigned short* e = (const unsigned short*)at;
     return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
   };
+  auto load_q = [&](int i) { return load_piece(q_row(i / kPieces) + i % kPieces * 8); };
+  const int most_rows = min(P::kRows, p.R * p.group - m0);  // (some of them may not count)
+  const int copies = kStreams == 2 || most_rows > 64 ? 1 : most_rows > 32 ? 2 : 4, copy_rows = 128 / copies;  // how often the rows are there
+  const int place = tid & 127, copy = place / copy_rows;  // a softmax thread's
+  constexpr int kEarly = C::kQInTmem ? kPieces : 4;  // pieces asked for early by a thread: its own row, or any
   uint4 early[kEarly];
-  const int most = (min(m0 + P::kRows, p.R * p.group) - m0) * kPieces;
   if (warp < C::kWarps) {
+    if constexpr (C::kQInTmem) {
+      const int m = place % copy_rows;
+      const __nv_bfloat16* at = q_row(min(m, most_rows - 1));
 #pragma unroll
-    for (int j = 0; j < kEarly; ++j)
-      if (tid + j * kSoftmaxThreads < most) early[j] = load_q(tid + j * kSoftmaxThreads);
+      for (int j = 0; j < kEarly; ++j) early[j] = load_piece(at + j * 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kEarly; ++j)
+        if (tid + j * kSoftmaxThreads < most_rows * kPieces) early[j] = load_q(tid + j * kSoftmaxThreads);
+    }
   }
 
   int rows = p.row_counts ? p.row_counts[b] : p.R;
@@ -307,8 +334,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   rows = max(0, min(rows, p.R));
   const int m1 = max(m0, min(m0 + P::kRows, rows * p.group));  // (no rows: the same for every block of the cluster)
   const int r0 = m0 / p.group, r1 = max(r0, (m1 - 1) / p.group + 1);
-  // how often the rows are there, and the warps of each stream with rows
-  const int copies = kStreams == 2 || m1 - m0 > 64 ? 1 : m1 - m0 > 32 ? 2 : 4, copy_rows = 128 / copies;
+  // the warps of each stream with rows
   const int warps0 = copies > 1 && m1 > m0 ? 4 : (min(m1 - m0, 128) + 31) / 32;
   const int warps1 = kStreams == 1 ? 0 : (max(m1 - m0 - 128, 0) + 31) / 32;
   int min_depth = r0;
@@ -321,8 +347,8 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   const int t0 = (int)((int64_t)all_tiles * part / p.split), t1 = (int)((int64_t)all_tiles * (part + 1) / p.split);
   const int tiles = t1 - t0;
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
-      barrier_init(&sh.half[i], (uint32_t)max(1, kStreams == 1 || i == 0 ? warps0 : warps1));
+    for (int i = 0; i < kBuffers; ++i) {
+      if (kStreams == 2) barrier_init(&sh.half[i], (uint32_t)max(1, i == 0 ? warps0 : warps1));
       barrier_init(&sh.weights[i], (uint32_t)max(1, kStreams == 1 || i == 0 ? warps0 : warps1));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -362,11 +388,12 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   };
   if (warp >= C::kWarps) {
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersOthers));
-    if (warp == kCopies || warp == kCopies + 1) {
+    if (warp < kProducts) {
       // ---- copies of keys, of values: a lane has a box (`box` slots by 64 elements) of every tile, or the two of its
       // slots.  64 entries of the block table are in the warp's registers, the later 32 asked for 32 pages before
       // they are needed.  All that a tile's copies need is worked out before the wait for their place.
-      const bool values = warp != kCopies;
+      const bool values = (warp - kCopies) & 1;
+      constexpr int kStep = C::kCopyWarps / 2;  // warps that take turns at the tiles of keys, of values
       const CUtensorMap* map = values ? &v_map : &k_map;
       char* const places = values ? value_ring : key_ring;
       Ring& ring = sh.ring[values];
@@ -383,9 +410,9 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         far = entry(from + 32 + lane);
       };
       if (tiles > 0) refill(page_of(p, tile_start<kN>(keys, t0)));
-      int stage = 0, t = 0;
+      int t = (warp - kCopies) >> 1, stage = t;
       uint32_t parity = 1;  // of the ring's round before: nothing to wait for in the first
-      for (; t < tiles; ++t) {
+      for (; t < tiles; t += kStep) {
         const int start = tile_start<kN>(keys, t0 + t), end_entry = page_of(p, min(start + kN, p.capacity) - 1);
         if (end_entry >= first_entry + 64) {
           if (page_of(p, start) >= first_entry + 32 && end_entry < first_entry + 96) {
@@ -413,15 +440,15 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           if (boxes > 32) tma_box(to + kPanel, map, 64, token, kv_head, page, full);
         }
         __syncwarp();
-        if (++stage == kStages) {
-          stage = 0;
+        if ((stage += kStep) >= kStages) {
+          stage -= kStages;
           parity ^= 1;
         }
       }
       // every copy has landed before the block ends, even where the products gave up
       if (*(volatile uint32_t*)gave_up)
-        for (int x = max(0, t - kStages); x < t; ++x)
-          for (int i = 0; i < (1 << 22) && !barrier_try(&ring.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
+        for (int x = max(t - kStep, 0), n = 0; x >= 0 && n < kStages; x -= kStep, n += kStep)
+          for (int i = 0; i < (1 << 22) && x < tiles && !barrier_try(&ring.full[x % kStages], (uint32_t)(x / kStages) & 1); ++i) {
           }
       __syncwarp();
     } else if (warp == kProducts || (kStreams == 1 && warp == kProducts + 1)) {
@@ -442,7 +469,9 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         if (leader) {
 #pragma unroll
           for (int j = 0; j < D / 16; ++j)
-            mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4),
+            if constexpr (C::kQInTmem)
+              mma_tmem(tmem + buffer * kN, tmem + P::kQColumn + j * 8, k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4), kScores, j > 0);
+            else mma_shared(tmem + buffer * kN, a + (uint32_t)(((j >> 2) * kQPanel + (j & 3) * 32) >> 4),
                        k + (uint32_t)(((j >> 2) * kPanel + (j & 3) * 32) >> 4), kScores, j > 0);
           mma_commit(&sh.scores[buffer]);
           if (s == streams - 1) mma_commit(&sh.ring[0].empty[key_stage]);
@@ -470,22 +499,34 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       if constexpr (kStreams == 1) {
         if (warp == kProducts) {
           ok = barrier_wait(&sh.q_there, 0, gave_up);
+          int buffer = 0;
+          uint32_t round = 1;  // parity of the round of buffers before
           for (int t = 0; ok && t < tiles; ++t) {
             // (the weights that were in this buffer are used up)
-            if (t >= 2) ok = barrier_wait(&sh.rest[t & 1], (uint32_t)(t / 2 - 1) & 1, gave_up);
-            ok = ok && score(0, t & 1);
+            if (t >= kBuffers) ok = barrier_wait(&sh.rest[buffer], round, gave_up);
+            ok = ok && score(0, buffer);
+            if (++buffer == kBuffers) {
+              buffer = 0;
+              round ^= 1;
+            }
           }
         } else if (tiles > 0) {
+          int buffer = 0;
+          uint32_t round = 0;
           for (int t = 0; t < tiles; ++t) {
-            ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up) &&
-                 barrier_wait(&sh.weights[t & 1], (uint32_t)(t >> 1) & 1, gave_up);
+            ok = barrier_wait(&sh.ring[1].full[value_stage], value_parity, gave_up) && barrier_wait(&sh.weights[buffer], round, gave_up);
             if (!ok) break;
-            output(0, t, t & 1, 0);
+            output(0, t, buffer, 0);
+            if (kN == 128) output(0, t, buffer, 4);
             if (leader) {
-              mma_commit(&sh.rest[t & 1]);
+              mma_commit(&sh.rest[buffer]);
               mma_commit(&sh.ring[1].empty[value_stage]);
             }
             __syncwarp();
+            if (++buffer == kBuffers) {
+              buffer = 0;
+              round ^= 1;
+            }
             if (++value_stage == kStages) {
               value_stage = 0;
               value_parity ^= 1;
@@ -525,7 +566,22 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   } else {
     // ---- softmax: a thread has one row
     if constexpr (kStreams == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Many<D>::kRegistersSoftmax));
-    {  // rows of q that are not there stay as they are: their scores go nowhere
+    if constexpr (C::kQInTmem) {
+#pragma unroll
+      for (int j = 0; j < kPieces; j += 8) {
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          w[4 * i] = early[j + i].x ^ flip;
+          w[4 * i + 1] = early[j + i].y ^ flip;
+          w[4 * i + 2] = early[j + i].z ^ flip;
+          w[4 * i + 3] = early[j + i].w ^ flip;
+        }
+        tmem_store(tmem + ((uint32_t)((warp & 3) * 32) << 16) + P::kQColumn + j * 4, w);
+      }
+      tmem_stored();
+      before_sync();
+    } else {  // rows of q that are not there stay as they are: their scores go nowhere
       const int pieces = (m1 - m0) * kPieces;
       auto store_q = [&](int i, const uint4& x) {  // in the operand's layout
         const int m = i / kPieces, c = i % kPieces;
@@ -538,15 +594,15 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         if (tid + j * kSoftmaxThreads < pieces) store_q(tid + j * kSoftmaxThreads, early[j]);
       for (int i = tid + kEarly * kSoftmaxThreads; i < pieces; i += kSoftmaxThreads) store_q(i, load_q(i));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) barrier_arrive(&sh.q_there);
     }
+    __syncwarp();
+    if (lane == 0) barrier_arrive(&sh.q_there);
     const int s = warp >> 2, quarter = warp & 3, my_warps = s ? warps1 : warps0;
-    const int place = quarter * 32 + lane, copy = place / copy_rows, m = m0 + s * 128 + place % copy_rows;
+    const int m = m0 + s * 128 + place % copy_rows;
     float top = -INFINITY, sum = 0.f;  // the maximum that the row's weights were formed with, their sum
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, output = tmem + lanes + P::kOutputs + s * D;
 
-    // The tiles of keys, W = 64 / copies slots of each.
+    // The tiles of keys, W = kN / copies slots of each.
     auto all_tiles_of = [&](auto width) {
       constexpr int W = decltype(width)::value;
       const float scale = fabsf(p.scale_log2);
@@ -559,10 +615,12 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       const int first_m = m0 + s * 128, last_m = min(first_m + 128, m1) - 1;
       const int all_hi = min(keys.hi, p.tree ? ctx : ctx + first_m / p.group + 1);
       const int all_lo = p.window ? ctx + (p.tree ? p.R - 1 : last_m / p.group) - p.window + 1 : 0;
+      int buffer = s;
+      uint32_t round = 0;  // parity of the buffer's turn
       for (int t = 0; t < tiles; ++t) {
-        const int tile_at = tile_start<kN>(keys, t0 + t), start = tile_at + copy * W, buffer = kStreams == 1 ? t & 1 : s;
+        const int tile_at = tile_start<kN>(keys, t0 + t), start = tile_at + copy * W;
         const uint32_t scores = tmem + lanes + buffer * kN;
-        if (!barrier_wait(&sh.scores[buffer], (uint32_t)(kStreams == 1 ? t >> 1 : t) & 1, gave_up)) break;
+        if (!barrier_wait(&sh.scores[buffer], round, gave_up)) break;
         after_sync();
         uint32_t x[W];
         if constexpr (W == 16) {
@@ -626,7 +684,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           // The output has to be at rest.  (In Many it is: this tile's scores come after the product with the last
           // weights.)
           if (kStreams == 1) {
-            if (!barrier_wait(&sh.rest[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1, gave_up)) break;
+            if (!barrier_wait(&sh.rest[buffer ? buffer - 1 : kBuffers - 1], buffer ? round : round ^ 1, gave_up)) break;
             after_sync();
           }
           const float f = rise ? power_of_two(top - now) : 1.0f;
@@ -660,7 +718,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
           }
           if constexpr (W == 16) tmem_store_8(scores + copy * W / 2, w);
           else tmem_store_16(scores + (copy * W + c0) / 2, w);
-          if (kN == 128 && c0 == 32) {
+          if (kStreams == 2 && c0 == 32) {
             tmem_stored();
             before_sync();
             __syncwarp();
@@ -684,13 +742,19 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
         before_sync();
         __syncwarp();
         if (lane == 0) barrier_arrive(&sh.weights[buffer]);
+        if (kStreams == 2) {
+          round ^= 1;
+        } else if (++buffer == kBuffers) {
+          buffer = 0;
+          round ^= 1;
+        }
       }
     };
     if (quarter < my_warps) {
       if constexpr (kStreams == 1) {
-        if (copies == 4) all_tiles_of(std::integral_constant<int, 16>());
-        else if (copies == 2) all_tiles_of(std::integral_constant<int, 32>());
-        else all_tiles_of(std::integral_constant<int, 64>());
+        if (copies == 4) all_tiles_of(std::integral_constant<int, kN / 4>());
+        else if (copies == 2) all_tiles_of(std::integral_constant<int, kN / 2>());
+        else all_tiles_of(std::integral_constant<int, kN>());
       } else {
         all_tiles_of(std::integral_constant<int, kN>());
       }
@@ -869,11 +933,11 @@ TensorBuild tensor_build() {
   return {(const void*)attention_tensor_kernel<C>, Plan<C>::kSmem, Plan<C>::kRows, C::kThreads, C::kN};
 }
 
-// What a build needs before its first launch on a device; clusters[i]: how many clusters of 2^i blocks, i <= 4, the
+// What a build needs before its first launch on a device; clusters[n]: how many clusters of n blocks, n <= 16, the
 // device holds at a time.
 int prepare_build(const TensorBuild& k, int at, const int** clusters) {
   static std::mutex m;
-  static int known[6][64][5];
+  static int known[6][64][17];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(e);
@@ -884,8 +948,8 @@ int prepare_build(const TensorBuild& k, int at, const int** clusters) {
     e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
     if (e != cudaSuccess) return cuda_fail(e);
     (void)cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    for (int i = 1; i <= 4; ++i) {
-      Launch l(dim3(1u << i, 1, 1), (unsigned)k.threads, (size_t)k.smem, nullptr, 1u << i);
+    for (int i = 2; i <= 16; ++i) {
+      Launch l(dim3((unsigned)i, 1, 1), (unsigned)k.threads, (size_t)k.smem, nullptr, (unsigned)i);
       l.cfg.attrs = &l.at[1];  // (the cluster's size alone)
       l.cfg.numAttrs = 1;
       if (cudaOccupancyMaxActiveClusters(&n[i], k.kernel, &l.cfg) != cudaSuccess) n[i] = 0;
@@ -926,9 +990,10 @@ int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st
     if (p.window && reach > (int64_t)p.window + p.sinks + p.R) reach = (int64_t)p.window + p.sinks + p.R;
     const int64_t tiles = (reach + k.slots - 1) / k.slots;
     p.split = 1;
-    for (int i = 1; i <= 4 && units << i <= sms && 1 << i <= tiles && units <= clusters[i]; ++i) p.split = 1 << i;
+    for (int n = 2; n <= 16 && units * n <= sms && n <= tiles; ++n)
+      if (units <= clusters[n]) p.split = n;
   }
-  while (p.split > 1 && !clusters[__builtin_ctz(p.split)]) p.split /= 2;
+  while (p.split > 1 && !clusters[p.split]) --p.split;
   note_launch("attention_tensor_kernel<%d, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows, boxes of %d", p.dim, k.rows,
               k.threads, p.row_tiles * p.split, p.heads, p.B, p.split, box);
   Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), (unsigned)k.threads, (size_t)k.smem, st, (unsigned)p.split);

@@ -63,7 +63,7 @@ def test_shapes(ersd, dtype, D, page, Hq, H):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("R,ctx", [(1, 0), (1, 1), (1, 127), (1, 128), (2, 126), (1, 2000), (16, 63), (17, 64), (33, 500), (64, 0), (130, 70),
                                    (300, 1), (257, 255)])
-@pytest.mark.parametrize("split", [0, 1, 2, 8])
+@pytest.mark.parametrize("split", [0, 1, 3, 8])
 def test_lengths(ersd, dtype, R, ctx, split):
     check(ersd, *make(2, R, 8, 2, 64, 16, [ctx, ctx // 2], dtype), split=split)
 

@@ -26,7 +26,7 @@ def test_attention_and_cache(ersd):
                      ((z(64).expand(1, 3, 4, 64), k, v, table, lens, out), {})]:
         with pytest.raises((ValueError, TypeError)):
             f(*args, **kw)
-    for kw in (dict(window=-1), dict(parent=[-1, 0, 2]), dict(split=3), dict(kernel_path=7)):
+    for kw in (dict(window=-1), dict(parent=[-1, 0, 2]), dict(split=17), dict(kernel_path=7)):
         with pytest.raises(ersd.ErsdError) as e:
             f(q, k, v, table, lens, out, **kw)
         assert e.value.status == -1, kw

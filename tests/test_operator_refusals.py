@@ -97,7 +97,7 @@ def test_attention(L):
     for p in keep:
         assert call(o=opts(ChunkOpts, parent=C.cast(p, C.c_void_p))) == EINVAL
     assert call(o=opts(ChunkOpts, parent=C.cast(star, C.c_void_p)), R=300) == EUNSUP
-    for bad in (dict(window=-1), dict(sinks=-1), dict(max_context=-1), dict(split=3), dict(split=32), dict(split=-1), dict(kernel_path=3),
+    for bad in (dict(window=-1), dict(sinks=-1), dict(max_context=-1), dict(split=17), dict(split=32), dict(split=-1), dict(kernel_path=3),
                 dict(scale=math.nan), dict(scale=math.inf)):
         assert call(o=opts(ChunkOpts, **bad)) == EINVAL, bad
     assert call(o=opts(ChunkOpts, row_counts=P + 2)) == EALIGN
