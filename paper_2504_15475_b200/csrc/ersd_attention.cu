@@ -1,10 +1,16 @@
-// ersd_chunk_attention: checks, the choice of the kernel, and the kernel of 32-bit arithmetic.
+// ersd_chunk_attention: checks, the choice of the kernel, and the kernels of 32-bit arithmetic.
 //
-// The kernel of 32-bit arithmetic takes a tile of MR packed rows of one kv head through the keys, kNK slots at a
-// time: keys and values are copied to shared memory as floats, a thread forms the scores of one slot with several
-// rows, the softmax's running maximum and sum live in shared memory, and a thread holds four columns of a few
-// rows of the output in registers.  `split` thread blocks of a cluster share the keys of a tile of rows and join
-// their partial results through distributed shared memory, so that a few rows over a long cache use many SMs.
+// Up to 32 packed rows (see AttentionParams), where the cache's bytes bound the call: rows_kernel takes four or eight.
+// L lanes share a slot, eight elements of its key and value in registers each, so that a warp has 32 / L slots at a
+// time and every warp goes through its own slots without waiting for another: the lanes' parts of the scores are
+// summed and dealt out by a few exchanges (lane r ends with row r's), lane r weighs row r's, and each lane adds its
+// part of the value to its part of the outputs.  What the slots' lanes, the warps and, with
+// `split` blocks to a cluster, the blocks have is joined at the end through shared memory.
+//
+// More rows, where the multiplications do: tile_kernel takes 64 rows through the keys, kNK slots at a time: keys and
+// values are copied to shared memory as floats, a thread forms the scores of four slots with four rows, the
+// softmax's running maximum and sum live in shared memory, and a thread holds four columns of several rows of the
+// output in registers.  `split` blocks join their partial results through distributed shared memory.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math.h>
@@ -50,10 +56,34 @@ __device__ __forceinline__ float4 four(const T* at, int left, bool wide) {
   return f;
 }
 
+// Whether row r (-1: none) sees a slot; `above`: a tree's nodes that it sees.
+__device__ __forceinline__ bool sees(const AttentionParams& p, const KeyRange& keys, int ctx, int slot, int r, const uint32_t* above) {
+  if (r < 0 || slot >= keys.hi) return false;
+  if (!p.tree) return slot <= ctx + r && (!p.window || slot > ctx + r - p.window || slot < p.sinks);
+  if (slot < ctx) return !p.window || slot > ctx + (int)p.depth[r] - p.window || slot < p.sinks;
+  const int node = slot - ctx;
+  return above[node >> 5] >> (node & 31) & 1u;
+}
+// The nodes of a tree that row r sees.
+__device__ __forceinline__ void nodes_above(const AttentionParams& p, int ctx, int r, uint32_t* above) {
+  uint32_t w[ERSD_MAX_ROWS / 32];
+#pragma unroll
+  for (int j = 0; j < ERSD_MAX_ROWS / 32; ++j) w[j] = 0;
+  if (r >= 0) {
+    for (int n = r;; n = p.parent[n]) {
+      const int pos = ctx + p.depth[n];
+      if (!p.window || p.depth[n] > (int)p.depth[r] - p.window || pos < p.sinks) w[n >> 5] |= 1u << (n & 31);
+      if (n == 0) break;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < ERSD_MAX_ROWS / 32; ++j) above[j] = w[j];
+}
+
 template <int MR, int DP>
 struct Shared {
-  float q[MR][DP];
-  float k[kNK][DP + 4];  // (+4: a warp's 16-byte reads of 32 slots fall on all banks)
+  float q[MR][DP + 4];   // (+4: a warp's 16-byte reads of several rows or slots fall on other banks)
+  float k[kNK][DP + 4];
   float v[kNK][DP];
   float s[MR][kNK + 4];
   float top[MR], sum[MR], factor[MR];  // running maximum, sum, and what the output is scaled by this tile
@@ -63,7 +93,7 @@ struct Shared {
 
 // MR packed rows, DP >= dim columns (a multiple of 64).
 template <typename T, int MR, int DP>
-__global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionParams p, bool wide) {
+__global__ void __launch_bounds__(kThreads) tile_kernel(const AttentionParams p, bool wide) {
   extern __shared__ __align__(16) char raw[];
   Shared<MR, DP>& sh = *(Shared<MR, DP>*)raw;
   const int tid = threadIdx.x, kv_head = blockIdx.y, b = blockIdx.z;
@@ -94,20 +124,7 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionPara
     sh.top[m] = -INFINITY;
     sh.sum[m] = 0.f;
     sh.factor[m] = 0.f;
-    if (p.tree) {
-      uint32_t w[ERSD_MAX_ROWS / 32];
-#pragma unroll
-      for (int j = 0; j < ERSD_MAX_ROWS / 32; ++j) w[j] = 0;
-      if (r >= 0) {
-        for (int n = r;; n = p.parent[n]) {
-          const int pos = ctx + p.depth[n];
-          if (!p.window || p.depth[n] > (int)p.depth[r] - p.window || pos < p.sinks) w[n >> 5] |= 1u << (n & 31);
-          if (n == 0) break;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < ERSD_MAX_ROWS / 32; ++j) sh.above[m][j] = w[j];
-    }
+    if (p.tree) nodes_above(p, ctx, r, sh.above[m]);
   }
   int min_depth = r0;
   if (p.tree) {
@@ -147,38 +164,37 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionPara
     }
     __syncthreads();
     {
-      constexpr int kParts = kThreads / kNK, kRows = MR / kParts;  // a thread: one slot, kRows rows
-      const int n = tid % kNK, part_of = tid / kNK, slot = start + n;
-      float s[kRows];
+      // a thread: slots x, x + 16, ..; rows 4 y to 4 y + 3
+      static_assert(MR == 64 && kNK == 64 && kThreads == 256, "");
+      const int x = tid & 15, y = tid >> 4;
+      float s[4][4];
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) s[i] = 0.f;
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
       for (int d = 0; d < DP; d += 4) {
-        const float4 fk = *(const float4*)&sh.k[n][d];
+        float4 fq[4], fk[4];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          const float4 fq = *(const float4*)&sh.q[part_of * kRows + i][d];
-          s[i] = fmaf(fq.x, fk.x, s[i]);
-          s[i] = fmaf(fq.y, fk.y, s[i]);
-          s[i] = fmaf(fq.z, fk.z, s[i]);
-          s[i] = fmaf(fq.w, fk.w, s[i]);
-        }
-      }
+        for (int i = 0; i < 4; ++i) fq[i] = *(const float4*)&sh.q[y * 4 + i][d];
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const int m = part_of * kRows + i, r = sh.row[m];
-        bool see = r >= 0 && slot < keys.hi;
-        if (see) {
-          if (!p.tree) {
-            see = slot <= ctx + r && (!p.window || slot > ctx + r - p.window || slot < p.sinks);
-          } else if (slot < ctx) {
-            see = !p.window || slot > ctx + (int)p.depth[r] - p.window || slot < p.sinks;
-          } else {
-            const int node = slot - ctx;
-            see = sh.above[m][node >> 5] >> (node & 31) & 1u;
+        for (int j = 0; j < 4; ++j) fk[j] = *(const float4*)&sh.k[x + 16 * j][d];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i][j] = fmaf(fq[i].x, fk[j].x, s[i][j]);
+            s[i][j] = fmaf(fq[i].y, fk[j].y, s[i][j]);
+            s[i][j] = fmaf(fq[i].z, fk[j].z, s[i][j]);
+            s[i][j] = fmaf(fq[i].w, fk[j].w, s[i][j]);
           }
-        }
-        sh.s[m][n] = see ? s[i] : -INFINITY;
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int m = y * 4 + i, n = x + 16 * j;
+          sh.s[m][n] = sees(p, keys, ctx, start + n, sh.row[m], sh.above[m]) ? s[i][j] : -INFINITY;
+        }
     }
     __syncthreads();
     // a warp takes whole rows: maximum, weights, sum
@@ -291,43 +307,283 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionPara
   }
 }
 
+// ---- few rows
+constexpr int kRowWarps = 4, kAhead = 2;  // kAhead: steps whose keys and values a warp asks for at once
+
+template <int L, int MR>
+struct RowShared {
+  static constexpr int kParts = kRowWarps * (32 / L), DP = 8 * L;
+  float o[kParts][MR][DP];
+  float top[kParts][MR], sum[kParts][MR];
+  float joined[MR][DP];
+  float joined_top[MR], joined_sum[MR];
+  int row[MR];
+  uint32_t above[MR][ERSD_MAX_ROWS / 32];
+};
+
+// Eight elements of a row from `at` on as floats; `wide`: on a boundary of 16 bytes (and the row goes on that far).
+template <typename T>
+__device__ __forceinline__ void eight(const T* at, int left, bool wide, float* f) {
+  if (wide && left >= 8) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 a = *(const float4*)at, b = *((const float4*)at + 1);
+      f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    } else {
+      const uint4 w = *(const uint4*)at;
+      const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(v[i] << 16);
+        f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < left ? as_float(at[i]) : 0.f;
+  }
+}
+
+// MR packed rows (4 or 8), heads of up to 8 L.
+template <typename T, int L, int MR>
+__global__ void __launch_bounds__(32 * kRowWarps, MR == 8 ? 3 : 4) rows_kernel(const AttentionParams p, bool wide) {
+  constexpr int kSlots = 32 / L, kTile = kSlots * kRowWarps * kAhead, DP = 8 * L;
+  extern __shared__ __align__(16) char raw[];
+  RowShared<L, MR>& sh = *(RowShared<L, MR>*)raw;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kv_head = blockIdx.y, b = blockIdx.z;
+  const int j = lane % L, g = lane / L, first_lane = lane - j;  // part of the slot's elements, slot of the step
+  const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  int rows = p.row_counts ? p.row_counts[b] : p.R;
+  const int ctx = max(0, p.context_lens[b]);
+  rows = max(0, min(rows, p.R));
+  const int m0 = tile * MR, m1 = min(m0 + MR, rows * p.group);
+  if (m0 >= m1) return;  // (the same for every block of the cluster)
+  const int r0 = m0 / p.group, r1 = (m1 - 1) / p.group + 1;
+  float q[MR][8];
+#pragma unroll
+  for (int m = 0; m < MR; ++m) {
+    const int r = (m0 + m) / p.group, h = kv_head * p.group + m0 + m - r * p.group;
+    const bool there = m0 + m < m1;
+    eight((const T*)p.q + b * p.q_b + (there ? r * p.q_r + h * p.q_h : 0) + j * 8, there ? p.dim - j * 8 : 0, wide, q[m]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[m][i] = there ? q[m][i] * p.scale_log2 : 0.f;
+  }
+  if (tid < MR) {
+    const int r = m0 + tid < m1 ? (m0 + tid) / p.group : -1;
+    sh.row[tid] = r;
+    if (p.tree) nodes_above(p, ctx, r, sh.above[tid]);
+  }
+  int min_depth = r0;
+  if (p.tree) {
+    min_depth = p.depth[r0];
+    for (int r = r0 + 1; r < r1; ++r) min_depth = min(min_depth, (int)p.depth[r]);
+  }
+  __syncthreads();
+  const KeyRange keys = key_range<kTile>(p, ctx, r1, min_depth);
+  const int t0 = (int)((int64_t)keys.tiles * part / p.split), t1 = (int)((int64_t)keys.tiles * (part + 1) / p.split);
+  const int32_t* table = p.table + b * p.table_stride;
+  const T* K = (const T*)p.k + kv_head * p.k_head + j * 8;
+  const T* V = (const T*)p.v + kv_head * p.v_head + j * 8;
+  const int my_row = sh.row[j & (MR - 1)];
+  const uint32_t* above = sh.above[j & (MR - 1)];
+  // step u of tile t: slot of this lane, and its page (-1: none, or no row sees it)
+  auto slot_of = [&](int t, int u) { return tile_start<kTile>(keys, t) + (u * kRowWarps + warp) * kSlots + g; };
+  auto page_at = [&](int t, int u) {
+    if (t >= t1) return -1;
+    const int slot = slot_of(t, u);
+    if (keys.dead(slot)) return -1;
+    const int page = table[page_of(p, slot)];
+    return page < p.num_pages ? max(page, -1) : -1;
+  };
+  float o[MR][8];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[m][i] = 0.f;
+  float top = -INFINITY, sum = 0.f;  // of row j & (MR - 1) over this lane's slots
+  int page[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) page[u] = page_at(t0, u);
+  for (int t = t0; t < t1; ++t) {
+    float k[kAhead][8], v[kAhead][8];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      // (slots that no row sees are not read: their values could be anything, and 0 * NaN is no 0)
+      const int slot = slot_of(t, u), token = page[u] < 0 ? 0 : slot - page_of(p, slot) * p.page_size, left = page[u] < 0 ? 0 : p.dim - j * 8;
+      const int64_t at = max(page[u], 0);
+      eight(K + at * p.k_page + token * p.k_token, left, wide, k[u]);
+      eight(V + at * p.v_page + token * p.v_token, left, wide, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) page[u] = page_at(t + 1, u);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int slot = slot_of(t, u);
+      float s[MR];
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        s[m] = q[m][0] * k[u][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s[m] = fmaf(q[m][i], k[u][i], s[m]);
+      }
+      // sums over the slot's lanes, row r's to lanes r, r + MR, ..
+#pragma unroll
+      for (int half = MR / 2; half; half >>= 1) {
+        const bool upper = j & half;
+#pragma unroll
+        for (int m = 0; m < half; ++m) {
+          const float send = upper ? s[m] : s[m + half], keep = upper ? s[m + half] : s[m];
+          s[m] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, half);
+        }
+      }
+#pragma unroll
+      for (int w = MR; w < L; w <<= 1) s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], w);
+      const float x = sees(p, keys, ctx, slot, my_row, above) ? s[0] : -INFINITY;
+      // the output is scaled only when a maximum has risen by more than 2^8: weights are then 2^8 at most
+      const bool rise = x > top + 8.0f;
+      if (__any_sync(0xFFFFFFFFu, rise)) {
+        const float f = rise ? exp2f(top - x) : 1.0f;
+        sum *= f;
+        if (rise) top = x;
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+          const float fm = __shfl_sync(0xFFFFFFFFu, f, first_lane + m);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[m][i] *= fm;
+        }
+      }
+      const float weight = exp2f(x - (top == -INFINITY ? 0.f : top));
+      sum += weight;
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        const float w = __shfl_sync(0xFFFFFFFFu, weight, first_lane + m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[m][i] = fmaf(w, v[u][i], o[m][i]);
+      }
+    }
+  }
+
+  // Join: out = sum_c 2^(top_c - top) o_c / sum_c 2^(top_c - top) sum_c over the slots' lanes and the warps ...
+  {
+    const int c = warp * kSlots + g;
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) *(float4*)&sh.o[c][m][j * 8 + i] = make_float4(o[m][i], o[m][i + 1], o[m][i + 2], o[m][i + 3]);
+    if (j < MR) {
+      sh.top[c][j] = top;
+      sh.sum[c][j] = sum;
+    }
+  }
+  __syncthreads();
+  auto write = [&](int m, int d, const float4& y, float total) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int r = (m0 + m) / p.group, h = kv_head * p.group + m0 + m - r * p.group;
+    T* out = (T*)p.out + b * p.o_b + r * p.o_r + h * p.o_h + d;
+    const float x[4] = {y.x * inv, y.y * inv, y.z * inv, y.w * inv};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (d + i < p.dim) out[i] = (T)x[i];
+  };
+  for (int i = tid; i < (m1 - m0) * (DP / 4); i += 32 * kRowWarps) {
+    const int m = i / (DP / 4), d = (i - m * (DP / 4)) * 4;
+    float most = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int c = 0; c < RowShared<L, MR>::kParts; ++c) most = fmaxf(most, sh.top[c][m]);
+    const float from = most == -INFINITY ? 0.f : most;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int c = 0; c < RowShared<L, MR>::kParts; ++c) {
+      const float theirs = sh.sum[c][m];
+      if (theirs == 0.f) continue;  // saw nothing
+      const float f = exp2f(sh.top[c][m] - from);
+      const float4 x = *(const float4*)&sh.o[c][m][d];
+      total = fmaf(f, theirs, total);
+      y.x = fmaf(f, x.x, y.x);
+      y.y = fmaf(f, x.y, y.y);
+      y.z = fmaf(f, x.z, y.z);
+      y.w = fmaf(f, x.w, y.w);
+    }
+    if (p.split == 1) {
+      write(m, d, y, total);
+    } else {
+      *(float4*)&sh.joined[m][d] = y;
+      sh.joined_top[m] = most;  // (all threads of the row the same)
+      sh.joined_sum[m] = total;
+    }
+  }
+  if (p.split == 1) return;
+  // ... and over the blocks of the cluster, whose warps share the rows.
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  for (int i = tid + part * 32 * kRowWarps; i < (m1 - m0) * (DP / 4); i += 32 * kRowWarps * p.split) {
+    const int m = i / (DP / 4), d = (i - m * (DP / 4)) * 4;
+    float most = -INFINITY, total = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < p.split; ++c) most = fmaxf(most, *cluster.map_shared_rank(&sh.joined_top[m], c));
+    const float from = most == -INFINITY ? 0.f : most;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = 0; c < p.split; ++c) {
+      const float theirs = *cluster.map_shared_rank(&sh.joined_sum[m], c), at = *cluster.map_shared_rank(&sh.joined_top[m], c);
+      const float4 x = *(const float4*)cluster.map_shared_rank(&sh.joined[m][d], c);
+      const float f = theirs == 0.f ? 0.f : exp2f(at - from);
+      total = fmaf(f, theirs, total);
+      y.x = fmaf(f, x.x, y.x);
+      y.y = fmaf(f, x.y, y.y);
+      y.z = fmaf(f, x.z, y.z);
+      y.w = fmaf(f, x.w, y.w);
+    }
+    write(m, d, y, total);
+  }
+  cluster.sync();  // (no block ends while another reads its shared memory)
+}
+
 struct Build {
   const void* kernel;
   size_t smem;
-  int rows;
+  int rows, threads, slots;
 };
 template <typename T, int MR>
-Build build_of(int dim) {
-  if (dim <= 64) return {(const void*)attention_kernel<T, MR, 64>, sizeof(Shared<MR, 64>), MR};
-  if (dim <= 128) return {(const void*)attention_kernel<T, MR, 128>, sizeof(Shared<MR, 128>), MR};
-  return {(const void*)attention_kernel<T, MR, 256>, sizeof(Shared<MR, 256>), MR};
+Build rows_build(int dim) {
+  constexpr int kThreadsFew = 32 * kRowWarps, kSlots = kRowWarps * kAhead;  // slots of a tile: times 32 / L
+  if (dim <= 64) return {(const void*)rows_kernel<T, 8, MR>, sizeof(RowShared<8, MR>), MR, kThreadsFew, kSlots * 4};
+  if (dim <= 128) return {(const void*)rows_kernel<T, 16, MR>, sizeof(RowShared<16, MR>), MR, kThreadsFew, kSlots * 2};
+  return {(const void*)rows_kernel<T, 32, MR>, sizeof(RowShared<32, MR>), MR, kThreadsFew, kSlots};
+}
+template <typename T>
+Build build_of(int64_t rows, int dim) {
+  if (rows <= 32) return rows <= 4 ? rows_build<T, 4>(dim) : rows_build<T, 8>(dim);
+  if (dim <= 64) return {(const void*)tile_kernel<T, 64, 64>, sizeof(Shared<64, 64>), 64, kThreads, kNK};
+  if (dim <= 128) return {(const void*)tile_kernel<T, 64, 128>, sizeof(Shared<64, 128>), 64, kThreads, kNK};
+  return {(const void*)tile_kernel<T, 64, 256>, sizeof(Shared<64, 256>), 64, kThreads, kNK};
 }
 
 int launch_attention_f32(AttentionParams& p, bool bf16, int max_context, cudaStream_t st) {
-  // Tiles of 16 packed rows where there are few: a tile of 64 would spend four times the arithmetic on rows that
-  // are not there.
   const bool few = (int64_t)p.R * p.group <= 32;
-  const Build k = bf16 ? (few ? build_of<__nv_bfloat16, 16>(p.dim) : build_of<__nv_bfloat16, 64>(p.dim))
-                       : (few ? build_of<float, 16>(p.dim) : build_of<float, 64>(p.dim));
+  const Build k = bf16 ? build_of<__nv_bfloat16>((int64_t)p.R * p.group, p.dim) : build_of<float>((int64_t)p.R * p.group, p.dim);
   p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
   if (!p.split) {
+    // three or four blocks to an SM (one or two of 64 rows), of eight steps at least
     int64_t reach = (int64_t)max_context + p.R;
     if (p.window && reach > (int64_t)p.window + p.sinks + p.R) reach = (int64_t)p.window + p.sinks + p.R;
-    const int64_t tiles = (reach + kNK - 1) / kNK;
+    const int64_t tiles = (reach + k.slots - 1) / k.slots;
     p.split = 1;
-    while (p.split < 8 && units * p.split < 2 * sm_count() && p.split * 2 <= tiles) p.split *= 2;
+    while (p.split < (few ? 16 : 8) && units * p.split * 2 <= (few ? 4 : 2) * sm_count() && p.split * (few ? 8 : 2) <= tiles) p.split *= 2;
   }
-  if (p.split > 8) p.split = 8;
+  if (p.split > 8 && !few) p.split = 8;  // (a block of 64 rows takes half of an SM's shared memory and more)
   cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem);
+  if (e == cudaSuccess && p.split > 8) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return cuda_fail(e);
-  note_launch("attention_kernel<%s, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows", bf16 ? "bf16" : "f32", k.rows, kThreads,
-              p.row_tiles * p.split, p.heads, p.B, p.split);
-  Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), kThreads, k.smem, st, (unsigned)p.split);
-  const int64_t align = bf16 ? 4 : 4;  // elements of a 16-byte (8-byte) read
+  note_launch("attention %s_kernel<%s, %d rows>: %d threads x (%d, %d, %d) blocks, %d to a tile of rows", few ? "rows" : "tile", bf16 ? "bf16" : "f32",
+              k.rows, k.threads, p.row_tiles * p.split, p.heads, p.B, p.split);
+  Launch l(dim3((unsigned)(p.row_tiles * p.split), (unsigned)p.heads, (unsigned)p.B), (unsigned)k.threads, k.smem, st, (unsigned)p.split);
+  // whether rows start on boundaries of the reads: four elements, or with few rows 16 bytes
   const int64_t all = p.q_b | p.q_r | p.q_h | p.k_page | p.k_token | p.k_head | p.v_page | p.v_token | p.v_head;
-  const size_t bytes = bf16 ? 8 : 16;
-  bool wide = all % align == 0 && aligned_to(p.q, bytes) && aligned_to(p.k, bytes) && aligned_to(p.v, bytes);
+  const size_t bytes = bf16 && !few ? 8 : 16;
+  bool wide = all % (int64_t)(bytes / (bf16 ? 2 : 4)) == 0 && aligned_to(p.q, bytes) && aligned_to(p.k, bytes) && aligned_to(p.v, bytes);
   void* args[] = {(void*)&p, (void*)&wide};
   e = cudaLaunchKernelExC(&l.cfg, k.kernel, args);
   return e == cudaSuccess ? ERSD_OK : cuda_fail(e);
