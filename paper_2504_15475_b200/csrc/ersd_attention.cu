@@ -1,6 +1,6 @@
 // ersd_chunk_attention: checks, the choice of the kernel, and the kernels of 32-bit arithmetic.
 //
-// Up to 32 packed rows (see AttentionParams), where the cache's bytes bound the call: rows_kernel takes four or eight.
+// Up to 48 packed rows (see AttentionParams), where the cache's bytes bound the call: rows_kernel takes four.
 // L lanes share a slot, eight elements of its key and value in registers each, so that a warp has 32 / L slots at a
 // time and every warp goes through its own slots without waiting for another: the lanes' parts of the scores are
 // summed and dealt out by a few exchanges (lane r ends with row r's), lane r weighs row r's, and each lane adds its
@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(kThreads) tile_kernel(const AttentionParams p,
 }
 
 // ---- few rows
-constexpr int kRowWarps = 4, kAhead = 2;  // kAhead: steps whose keys and values a warp asks for at once
+// (eight rows to a warp: 30 us instead of 24 for chains of five, for want of registers)
+constexpr int kRows = 4, kRowWarps = 4, kAhead = 2;  // kAhead: steps whose keys and values a warp asks for at once
 
 template <int L, int MR>
 struct RowShared {
@@ -343,9 +344,9 @@ __device__ __forceinline__ void eight(const T* at, int left, bool wide, float* f
   }
 }
 
-// MR packed rows (4 or 8), heads of up to 8 L.
+// MR packed rows, heads of up to 8 L.
 template <typename T, int L, int MR>
-__global__ void __launch_bounds__(32 * kRowWarps, MR == 8 ? 3 : 4) rows_kernel(const AttentionParams p, bool wide) {
+__global__ void __launch_bounds__(32 * kRowWarps, 4) rows_kernel(const AttentionParams p, bool wide) {
   constexpr int kSlots = 32 / L, kTile = kSlots * kRowWarps * kAhead, DP = 8 * L;
   extern __shared__ __align__(16) char raw[];
   RowShared<L, MR>& sh = *(RowShared<L, MR>*)raw;
@@ -540,6 +541,8 @@ __global__ void __launch_bounds__(32 * kRowWarps, MR == 8 ? 3 : 4) rows_kernel(c
   cluster.sync();  // (no block ends while another reads its shared memory)
 }
 
+constexpr int kFewRows = 48;  // (30 rows: 50 us against 99 of tile_kernel, whose tiles are of 64 whether the rows are there or not)
+
 struct Build {
   const void* kernel;
   size_t smem;
@@ -554,14 +557,14 @@ Build rows_build(int dim) {
 }
 template <typename T>
 Build build_of(int64_t rows, int dim) {
-  if (rows <= 32) return rows <= 4 ? rows_build<T, 4>(dim) : rows_build<T, 8>(dim);
+  if (rows <= kFewRows) return rows_build<T, kRows>(dim);
   if (dim <= 64) return {(const void*)tile_kernel<T, 64, 64>, sizeof(Shared<64, 64>), 64, kThreads, kNK};
   if (dim <= 128) return {(const void*)tile_kernel<T, 64, 128>, sizeof(Shared<64, 128>), 64, kThreads, kNK};
   return {(const void*)tile_kernel<T, 64, 256>, sizeof(Shared<64, 256>), 64, kThreads, kNK};
 }
 
 int launch_attention_f32(AttentionParams& p, bool bf16, int max_context, cudaStream_t st) {
-  const bool few = (int64_t)p.R * p.group <= 32;
+  const bool few = (int64_t)p.R * p.group <= kFewRows;
   const Build k = bf16 ? build_of<__nv_bfloat16>((int64_t)p.R * p.group, p.dim) : build_of<float>((int64_t)p.R * p.group, p.dim);
   p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
