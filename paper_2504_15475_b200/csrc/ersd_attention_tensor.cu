@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   }
   const KeyRange keys = key_range<kN>(p, ctx, r1, min_depth);
   const int all_tiles = m1 > m0 ? keys.tiles : 0;
-  const int t0 = (int)((int64_t)all_tiles * part / p.split), t1 = (int)((int64_t)all_tiles * (part + 1) / p.split);
+  const int t0 = all_tiles * part / p.split, t1 = all_tiles * (part + 1) / p.split;  // (at most 2^24 tiles, 16 parts)
   const int tiles = t1 - t0;
   if (tid == 0) {
     for (int i = 0; i < kBuffers; ++i) {
@@ -768,21 +768,23 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
       const int r = m / p.group, g = m - r * p.group, at = s * 128 + place;
       __nv_bfloat16* out = (__nv_bfloat16*)p.out + b * p.o_b + r * p.o_r + (kv_head * p.group + g) * p.o_h;
 #pragma unroll
-      for (int c0 = 0; c0 < D; c0 += 32) {
-        uint32_t o[32];
+      for (int c0 = 0; c0 < D; c0 += 64) {
+        uint32_t o[64];
         if (tiles > 0) {
           tmem_load(output + c0, o);
+          tmem_load(output + c0 + 32, o + 32);
           tmem_loaded();
         } else {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) o[c] = 0;
+          for (int c = 0; c < 64; ++c) o[c] = 0;
         }
+        if (m >= m1) continue;
         if (joins) {
 #pragma unroll
-          for (int c = 0; c < 32; c += 4) *(uint4*)(parts + at * P::kPartRow + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-        } else if (m < m1) {
+          for (int c = 0; c < 64; c += 4) *(uint4*)(parts + at * P::kPartRow + c0 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+        } else {
 #pragma unroll
-          for (int c = 0; c < 32; c += 8) {
+          for (int c = 0; c < 64; c += 8) {
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = pair(__uint_as_float(o[c + 2 * j]) * inv, __uint_as_float(o[c + 2 * j + 1]) * inv);
