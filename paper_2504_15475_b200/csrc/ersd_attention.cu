@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads) tile_kernel(const AttentionParams p,
   rows = max(0, min(rows, p.R));
   const int m0 = tile * MR, m1 = min(m0 + MR, rows * p.group);
   if (m0 >= m1) return;  // (the same for every block of the cluster)
-  const int ctx = max(0, p.context_lens[b]);
+  const int ctx = context_of(p, b);
   const int r0 = m0 / p.group, r1 = (m1 - 1) / p.group + 1;
 
   constexpr int kD4 = DP / 4;
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) rows_kernel(const Attention
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int rows = p.row_counts ? p.row_counts[b] : p.R;
-  const int ctx = max(0, p.context_lens[b]);
+  const int ctx = context_of(p, b);
   rows = max(0, min(rows, p.R));
   const int m0 = tile * MR, m1 = min(m0 + MR, rows * p.group);
   if (m0 >= m1) return;  // (the same for every block of the cluster)

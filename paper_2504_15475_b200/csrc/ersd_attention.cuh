@@ -41,6 +41,9 @@ __device__ __forceinline__ int page_of(const AttentionParams& p, int slot) {
 // p.split = 0: chosen there.
 __attribute__((visibility("hidden"))) int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st);
 
+// Positions before the rows of sequence b (with the rows' own, below 2^30, they stay below 2^31).
+__device__ __forceinline__ int context_of(const AttentionParams& p, int b) { return min(max(0, p.context_lens[b]), (1 << 30) - 1); }
+
 // What a tile of rows [r0, r1) of a sequence has to read: slots [0, sink_hi) and [lo, hi), in tiles of N slots
 // that start at multiples of N.
 struct KeyRange {

@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   }
 
   int rows = p.row_counts ? p.row_counts[b] : p.R;
-  const int ctx = max(0, p.context_lens[b]);
+  const int ctx = context_of(p, b);
   rows = max(0, min(rows, p.R));
   const int m1 = max(m0, min(m0 + P::kRows, rows * p.group));  // (no rows: the same for every block of the cluster)
   const int r0 = m0 / p.group, r1 = max(r0, (m1 - 1) / p.group + 1);

@@ -440,6 +440,7 @@ PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     o.struct_size = sizeof o;
     const int32_t* lens = small<int32_t>(a[4], {B}, kc, "context_lens");
     o.scale = a[6] == Py_None ? 0.0f : number(a[6]);
+    if (a[6] != Py_None && o.scale == 0.0f) refuse(PyExc_ValueError, "%s must not be 0", "scale");  // (the library's sign for none given)
     std::vector<int32_t> parent;
     if (a[7] != Py_None) {
       parent = parents(a[7], (int)q.size(1));

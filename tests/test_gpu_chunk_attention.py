@@ -122,6 +122,11 @@ def test_slots_that_do_not_exist(ersd, dtype):
     far = torch.tensor([400, 60], dtype=torch.int32, device="cuda")
     out = check(ersd, q, k, v, table[:, :7].contiguous(), far, window=30)
     assert (out[0] == 0).all()
+    for far in (2 ** 31 - 1, 2 ** 30):
+        out = torch.full_like(q, 7.0)
+        for window, zeros in ((0, False), (5, True)):
+            ersd.ersd_chunk_attention(q, k, v, table, torch.full_like(lens, far), out, window=window)
+            assert torch.isfinite(out).all() and (out == 0).all() == zeros
     table[0, 2], table[1, 3] = -5, 10 ** 9                                  # pages that do not exist: keys of zeros
     check(ersd, q, k, v, table, lens)
 

@@ -22,7 +22,7 @@ def test_attention_and_cache(ersd):
                      ((q, k, v, table, lens[:0], out), {}), ((q, k, v, table, lens.cpu(), out), {}), ((q[..., :32], k, v, table, lens, out), {}),
                      ((q, k, v, table, lens, out[:, :2]), {}), ((q[0], k, v, table, lens, out), {}), ((q.transpose(2, 3), k, v, table, lens, out), {}),
                      ((z(2, 3, 4, 64), k, v, table, lens, out), {}), ((q, k[None], v[None], table, lens, out), {}),
-                     ((q, k, v, table, lens, out), dict(parent=[-1, 0])), ((q, k, v, table, lens, out), dict(row_counts=lens.float())),
+                     ((q, k, v, table, lens, out), dict(parent=[-1, 0])), ((q, k, v, table, lens, out), dict(row_counts=lens.float())), ((q, k, v, table, lens, out), dict(scale=0.0)),
                      ((z(64).expand(1, 3, 4, 64), k, v, table, lens, out), {})]:
         with pytest.raises((ValueError, TypeError)):
             f(*args, **kw)

@@ -68,6 +68,21 @@ def test_vocabularies(ersd, dtype, V, in_place):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [3, 100, 4095, 4097, 9000, 9001])
+def test_in_place_without_a_mask(ersd, dtype, V):
+    """Tokens that nothing changes are neither read nor written: what they hold stays, NaN among it."""
+    for parent, history in ((None, 30), ([-1, 0, 0, 2], 9000)):
+        x, a = make(3, 4, V, dtype, parent=parent, history=history, seed=11)
+        a["mask"] = None
+        check(ersd, torch.nan_to_num(x, nan=1.0), a, in_place=True)
+        y = x.cuda()
+        before = y.clone()
+        ersd.ersd_process_logits(y, y)
+        assert torch.equal(y.view(torch.int16 if dtype == torch.bfloat16 else torch.int32),
+                           before.view(torch.int16 if dtype == torch.bfloat16 else torch.int32))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("left_out", range(len(PARTS)))
 def test_parts_can_be_left_out(ersd, dtype, left_out):
     x, a = make(2, 5, 700, dtype, parent=[-1, 0, 0, 1, 1])
