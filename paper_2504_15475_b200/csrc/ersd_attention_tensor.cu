@@ -971,7 +971,7 @@ int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st
   const bool many = (int64_t)p.R * p.group > 128;
   p.row_tiles = (int)(((int64_t)p.R * p.group + (many ? 255 : 127)) / (many ? 256 : 128));
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
-  // Blocks with a long ring while no more than one goes to an SM (one token over 64000 positions: XX against 107 us),
+  // Blocks with a long ring while no more than one goes to an SM (18 sequences of 64000 positions, 144 blocks: 620 us; 1150 with the shorter rings and one block to an SM),
   // else two to an SM.
   const bool alone = many || units * (p.split ? p.split : 1) <= sms;
   const int at = (p.dim == 64 ? 0 : 3) + (many ? 2 : alone ? 1 : 0);
