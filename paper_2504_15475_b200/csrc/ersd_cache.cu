@@ -30,28 +30,41 @@ __device__ __forceinline__ int64_t slot_offset(const CacheParams& p, const Side&
   return page * s.page + ((int)at - entry * p.page_size) * s.token;
 }
 
-// Rows of one sequence (blockIdx.y): a thread copies a piece of a row's keys and the same piece of its values.
+constexpr int kAtOnce = 2;  // pieces of keys, and of values, that a thread asks for before it writes the first
+
+// Rows of one sequence (blockIdx.y): a thread copies pieces of rows' keys and the same pieces of their values.
 template <typename Piece>
 __global__ void __launch_bounds__(256) cache_append_kernel(const CacheParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int b = blockIdx.y;
+  const int b = blockIdx.y, per_row = p.heads * p.pieces;
+  const int64_t i0 = (int64_t)blockIdx.x * (256 * kAtOnce) + threadIdx.x;
   int rows = p.row_counts ? p.row_counts[b] : p.R;
   rows = max(0, min(rows, p.R));
   const int64_t ctx = max(0, p.context_lens[b]);
   const int32_t* table = p.table + b * p.table_stride;
-  const int per_row = p.heads * p.pieces;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int r = (int)(i / per_row);
-  if (r >= rows) return;
-  const int x = (int)(i - (int64_t)r * per_row), h = x / p.pieces, d = x - h * p.pieces;
-  Piece v[2];
+  Piece v[kAtOnce][2];
+  int r[kAtOnce], h[kAtOnce], d[kAtOnce];
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
-    v[s] = ((const Piece*)(p.side[s].rows + b * p.side[s].row_b + r * p.side[s].row_r + h * p.side[s].row_h))[d];
+  for (int k = 0; k < kAtOnce; ++k) {
+    const int64_t i = i0 + 256 * k;
+    // (a 64-bit division takes longer than the copy)
+    r[k] = i < 0x7FFFFFFF ? (int)i / per_row : (int)min(i / per_row, (int64_t)p.R);
+    const int x = (int)(i - (int64_t)r[k] * per_row);
+    h[k] = x / p.pieces;
+    d[k] = x - h[k] * p.pieces;
+    if (r[k] >= rows) continue;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int64_t at = slot_offset(p, p.side[s], table, ctx + r);
-    if (at >= 0) ((Piece*)(p.side[s].cache + at + h * p.side[s].head))[d] = v[s];
+    for (int s = 0; s < 2; ++s)
+      v[k][s] = ((const Piece*)(p.side[s].rows + b * p.side[s].row_b + r[k] * p.side[s].row_r + h[k] * p.side[s].row_h))[d[k]];
+  }
+#pragma unroll
+  for (int k = 0; k < kAtOnce; ++k) {
+    if (r[k] >= rows) continue;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int64_t at = slot_offset(p, p.side[s], table, ctx + r[k]);
+      if (at >= 0) ((Piece*)(p.side[s].cache + at + h[k] * p.side[s].head))[d[k]] = v[k][s];
+    }
   }
 }
 
@@ -156,7 +169,7 @@ extern "C" int ersd_cache_append(const ersd_cache* cache, const void* k_new, con
   const bool wide = pieces_of_16(p.side[0], d * size) && pieces_of_16(p.side[1], d * size);
   p.pieces = (int)(wide ? d * size / 16 : d);
   const auto kernel = wide ? cache_append_kernel<uint4> : size == 2 ? cache_append_kernel<uint16_t> : cache_append_kernel<uint32_t>;
-  const int64_t blocks = ((int64_t)R * c.heads * p.pieces + 255) / 256;
+  const int64_t blocks = ((int64_t)R * c.heads * p.pieces + 256 * kAtOnce - 1) / (256 * kAtOnce);
   if (blocks > 0x7FFFFFFF || (int64_t)c.heads * p.pieces > 0x7FFFFFFF) return ERSD_EUNSUPPORTED;
   note_launch("cache_append_kernel<%s>: 256 threads x (%lld, %d) blocks", wide ? "16 bytes" : "an element", (long long)blocks, B);
   Launch l(dim3((unsigned)blocks, (unsigned)B, 1), 256, 0, (cudaStream_t)cuda_stream);
