@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     }
     __syncthreads();
   }
+  const double rep_inverse = 1.0 / (double)rep;
   const uint32_t count_bits = p.long_history ? kLongCount : kShortCount;
   // The logit x of the table's token `at` on row r.
   auto changed = [&](float x, int at, int r) {
@@ -268,7 +269,8 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
       seen |= c > 0;
     }
     if (seen) {
-      if (p.repetition) x = x > 0.0f ? __fdiv_rn(x, rep) : x * rep;
+      // (a product in 64 bits for the quotient: rounded once like it, without a branch between the two)
+      if (p.repetition) x = (float)((double)x * (x > 0.0f ? rep_inverse : (double)rep));
       if (c) x -= fmaf(freq, (float)c, pres);
     }
     if (e & kBiased) x += bias[(p.long_history ? bias_at[at] : e >> kBiasShift & 0xFFFFu) - 1];
