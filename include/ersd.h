@@ -482,7 +482,8 @@ typedef struct ersd_logit_opts {
  * biases the later entry counts.  A masked token is -inf whatever its logit; a row whose mask allows nothing is
  * all -inf, for which a race yields token -1.
  *   logits device [B, R, V]   out device [B, R, V] of the same type: other memory, or `logits`
- *   itself with the same row stride (tokens that nothing changes are then neither read nor written)
+ *   itself with the same row stride (without a mask, tokens that nothing changes are then neither read nor
+ *   written)
  * Entries V..ld-1 of a row are left alone.
  * Errors: ERSD_EINVAL (null pointers, sizes < 1, strides below V, draft_tokens or parent that do not
  * go with R, values without tokens, ...); ERSD_EALIGN; ERSD_EUNSUPPORTED for B or R > 65535, draft

@@ -1045,6 +1045,6 @@ int ersd_last_cuda_error(void) { return g_last_cuda_error; }
 
 const char* ersd_last_launch(void) { return g_last_launch; }
 
-int ersd_version(void) { return 112; }
+int ersd_version(void) { return 113; }
 
 }  // extern "C"

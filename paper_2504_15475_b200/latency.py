@@ -2,6 +2,7 @@
 
     python -m paper_2504_15475_b200.latency [--V 128256] [--k 5] [--batches 1,2,4,8,16,32]
     python -m paper_2504_15475_b200.latency --trees [--batches 1,2,4]     # draft trees, batch drafting
+    python -m paper_2504_15475_b200.latency --operators [--context 4000]  # attention, cache, logits of draft trees
 
 Calls of a few rows are bound by latency, not by bandwidth, and a Python caller cannot issue
 them faster than about ten microseconds apart; so the calls are captured into a CUDA graph (30
@@ -119,6 +120,49 @@ def time_batch_drafting(args, c=8):
                               "timing": "CUDA graph replay, 30 calls per graph"}), flush=True)
 
 
+def time_operators(args, Hq=32, H=8, D=128, page=16, layers=32):
+    """The calls around a tree verification: a step's rows into the cache, their attention, logits, the accepted path."""
+    V, parent = args.V, wl.TREE_4x4
+    n = len(parent)
+    for B in [int(x) for x in args.batches.split(",")]:
+        gen = torch.Generator(device="cuda").manual_seed(4000 + B)
+        per = -(-(args.context + n) // page)
+        k, v = (torch.randn(B * per, page, H, D, generator=gen, device="cuda").bfloat16() for _ in range(2))
+        table = torch.randperm(B * per, generator=gen, device="cuda").view(B, per).to(torch.int32)
+        lens = torch.full((B,), args.context, dtype=torch.int32, device="cuda")
+        q = torch.randn(B, n, Hq, D, generator=gen, device="cuda").bfloat16()
+        new = torch.randn(2, B, n, H, D, generator=gen, device="cuda").bfloat16()
+        out = torch.empty_like(q)
+        # one accepted path of three nodes for every sequence, through all layers of a short cache
+        deep = torch.zeros(2, layers, B * 3, page, H, D, dtype=torch.bfloat16, device="cuda")
+        short = torch.arange(B * 3, dtype=torch.int32, device="cuda").view(B, 3)
+        few = torch.full((B,), 9, dtype=torch.int32, device="cuda")
+        path = torch.tensor([[0, 3, 7, 11, -1]], dtype=torch.int32, device="cuda").expand(B, 5).contiguous()
+        accept, after = torch.full((B,), 3, dtype=torch.int32, device="cuda"), torch.empty_like(few)
+        logits = torch.randn(B, n, V, generator=gen, device="cuda").bfloat16()
+        changed = torch.empty_like(logits)
+        history = torch.randint(0, V, (B, args.context), generator=gen, device="cuda", dtype=torch.int32)
+        drafts = torch.randint(0, V, (B, n), generator=gen, device="cuda", dtype=torch.int32)
+        rep = torch.full((B,), 1.1, device="cuda")
+        calls = (("ersd_cache_append", lambda i, st: binding.ersd_cache_append(new[0], new[1], k, v, table, lens, stream=st)),
+                 ("ersd_chunk_attention", lambda i, st: binding.ersd_chunk_attention(
+                     q, k, v, table, lens, out, parent=parent, max_context=args.context, stream=st)),
+                 ("ersd_process_logits", lambda i, st: binding.ersd_process_logits(
+                     logits, changed, history=history, draft_tokens=drafts, parent=parent, repetition=rep, stream=st)),
+                 ("ersd_cache_commit", lambda i, st: binding.ersd_cache_commit(
+                     deep[0], deep[1], short, few, path, accept, after, stream=st)))
+        for entry, call in calls:
+            if args.plain:
+                for i in range(args.plain):
+                    call(i, torch.cuda.current_stream())
+                torch.cuda.synchronize()
+                continue
+            call(0, torch.cuda.current_stream())
+            print(json.dumps({"entry": entry, "B": B, "nodes": n, "context": args.context, "V": V, "heads": [Hq, H, D], "dtype": "bf16",
+                              "launch": binding.ersd_last_launch(), "us_per_call": round(graph_time_us(call), 2),
+                              "timing": "CUDA graph replay, 30 calls per graph, the same inputs"}), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--V", type=int, default=128256)
@@ -128,6 +172,9 @@ def main():
     ap.add_argument("--split", type=int, default=0, help="thread blocks per row / per cluster (0: library default)")
     ap.add_argument("--trees", action="store_true",
                     help="time ersd_verify_tree on draft trees, and batch drafting, instead of the two entries above")
+    ap.add_argument("--operators", action="store_true",
+                    help="time the operators around a tree verification instead: attention, cache, logits")
+    ap.add_argument("--context", type=int, default=4000, help="positions before the rows (--operators)")
     ap.add_argument("--plain", type=int, default=0,
                     help="issue this many plain calls per case instead of replaying a graph and print no "
                          "times (for a profiler's launch list)")
@@ -136,6 +183,9 @@ def main():
     if not torch.cuda.is_available():
         raise SystemExit("needs a CUDA device")
     V, k = args.V, args.k
+    if args.operators:
+        time_operators(args)
+        return
     if args.trees:
         time_trees(args)
         time_batch_drafting(args)
