@@ -25,6 +25,8 @@ constexpr int kSlice = kLogitWarps * kChunk;
 constexpr int kLead = 8;              // most tokens a row's chunks start before the slice: see below
 constexpr int kSpan = kSlice + kLead;
 constexpr int kLists = kLogitWarps + 1;
+constexpr int kMany = 64;             // tokens with an entry from which on a chunk is shared, see below
+constexpr int kSharers = 1 + kLogitWarps;  // its own warp and those that have none
 // An entry of the table: how often the token occurs behind the prompt, and
 constexpr uint32_t kSeen = 1u << 31;     // that it is in the history
 constexpr uint32_t kDrafted = 1u << 30;  // that it is among the drafted tokens: its count depends on the row
@@ -93,6 +95,7 @@ struct LogitShared {
                                      // the frequent tokens, fall to different lanes)
   int32_t draft[ERSD_MAX_ROWS];
   uint8_t parent[ERSD_MAX_ROWS];
+  int listed[kLogitWarps];           // tokens of a warp's chunk that have an entry
   // behind it, where they are needed (room that is not taken lets more blocks onto an SM):
   //   uint32_t bias_at[kSpan];                              1 + index of the token's bias
   //   uint32_t mask[kLogitWarps][kMaskRing][2][32];         the one or two words in which a lane's bits are
@@ -110,11 +113,13 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   constexpr int kPer16 = 16 / (int)sizeof(T);
   const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int s0 = (int)blockIdx.y * kSlice;
+  // with few sequences several blocks share the rows: this one has `rows` of them from row0 on, which it counts from 0
+  const int row0 = (int)((int64_t)p.R * blockIdx.z / gridDim.z), rows = (int)((int64_t)p.R * (blockIdx.z + 1) / gridDim.z) - row0;
   // Chunks start on 16-byte boundaries of the input, `lead` tokens before the slice's own start.  Where all rows
   // have the same lead the table starts there, and a warp's chunk is a chunk of the table; else it starts kLead
   // before, and a warp's chunk of a row lies in two chunks of the table.
   auto lead_of = [&](int r) {
-    return (int)(((uintptr_t)((const T*)p.in + ((int64_t)b * p.R + r) * p.ld_in) / sizeof(T)) & (kPer16 - 1));
+    return (int)(((uintptr_t)((const T*)p.in + ((int64_t)b * p.R + row0 + r) * p.ld_in) / sizeof(T)) & (kPer16 - 1));
   };
   const int base = s0 - (kVary ? kLead : lead_of(0));
   const bool changes = p.history || p.draft_tokens || p.bias_count;
@@ -151,12 +156,12 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     return c;
   };
   const Piece first = piece_of(0);
-  const T* const in0 = (const T*)p.in + (int64_t)b * p.R * p.ld_in;
-  T* const out0 = (T*)p.out + (int64_t)b * p.R * p.ld_out;
-  const uint32_t* const mask0 = p.mask ? p.mask + b * p.mask_stride_b : nullptr;
+  const T* const in0 = (const T*)p.in + ((int64_t)b * p.R + row0) * p.ld_in;
+  T* const out0 = (T*)p.out + ((int64_t)b * p.R + row0) * p.ld_out;
+  const uint32_t* const mask0 = p.mask ? p.mask + b * p.mask_stride_b + row0 * p.mask_stride_r : nullptr;
   // This lane's 32 bits of row r's mask lie in one word or two, which are asked for kMaskRing - 1 rows ahead.
   auto ask_mask = [&](int r) {
-    if (p.mask && r < p.R) {
+    if (p.mask && r < rows) {
       const int bit = (kVary ? piece_of(r).start : first.start) + lane * 32, w = bit >> 5;
       const uint32_t* m = mask0 + r * p.mask_stride_r;
       const bool lo = w >= 0 && w < mask_words, hi = (bit & 31) && w + 1 >= 0 && w + 1 < mask_words;
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     asm volatile("cp.async.wait_group %0;" ::"n"(kMaskRing - kRing) : "memory");
 #pragma unroll
     for (int r = 0; r < kRing - 1; ++r)
-      if (r < p.R) load(r, bits_of(r));
+      if (r < rows) load(r, bits_of(r));
   }
 
   float rep = 1.0f, pres = 0.0f, freq = 0.0f;
@@ -259,13 +264,13 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   }
   const double rep_inverse = 1.0 / (double)rep;
   const uint32_t count_bits = p.long_history ? kLongCount : kShortCount;
-  // The logit x of the table's token `at` on row r.
+  // The logit x of the table's token `at` on the block's row r.
   auto changed = [&](float x, int at, int r) {
     const uint32_t e = sh.table[at];
     uint32_t c = e & count_bits;
     bool seen = (e & kSeen) != 0;
     if (e & kDrafted) {  // a drafted token counts if it is on the path to this row
-      for (int m = r; m > 0; m = p.tree ? sh.parent[m] : m - 1) c += sh.draft[m] == at + base;
+      for (int m = row0 + r; m > 0; m = p.tree ? sh.parent[m] : m - 1) c += sh.draft[m] == at + base;
       seen |= c > 0;
     }
     if (seen) {
@@ -280,12 +285,12 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   if (p.in_place && !p.mask) {  // the listed tokens alone
     if (!changes) return;
     for (int l = warp; l < kLists; l += 2 * kLogitWarps) {
-      for (int r = 0; r < p.R; ++r) {
+      for (int r = 0; r < rows; ++r) {
         const int lead = lead_of(r);
         for (uint32_t left = sh.touched[l][lane]; left; left &= left - 1) {
           const int at = l * kChunk + lane + 32 * (__ffs(left) - 1), t = at + base;
           if (t < s0 - lead || t >= s0 - lead + kSlice) continue;  // (in this row the token is in another block's slice)
-          T* x = (T*)p.out + ((int64_t)b * p.R + r) * p.ld_out + t;
+          T* x = out0 + r * p.ld_out + t;
           *x = from_float<T>(changed(to_float(*x), at, r));
         }
       }
@@ -293,34 +298,72 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     return;
   }
 
-  if (!streams) return;
-  const uint32_t my_touched = changes ? sh.touched[warp][lane] : 0u;
-  for (int r = 0; r < p.R; ++r) {
+  // A sequence's frequent tokens lie close together.  Of the chunk with the most of them, from kMany on, the warps
+  // without a chunk take their share in every row, or its own warp would hold up the block (4 us for each row with
+  // histories of 3000 tokens).
+  int shared_chunk = -1;
+  if (changes) {
+    if (warp < kLogitWarps) {
+      const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(sh.touched[warp][lane]));
+      if (lane == 0) sh.listed[warp] = n;
+    }
+    __syncthreads();
+    int most = kMany - 1;
+#pragma unroll
+    for (int w = 0; w < kLogitWarps; ++w)
+      if (sh.listed[w] > most) most = sh.listed[w], shared_chunk = w;
+  }
+  // The tokens of list l, of every `step`-th 32 from `from` on, in a chunk of row r.
+  auto change_listed = [&](T* x, int chunk_start, int l, int from, int step, int r) {
+    uint32_t mine = sh.touched[l][lane];
+    if (step > 1) {
+      uint32_t pattern = 0;
+#pragma unroll
+      for (int i = 0; i < 32; i += kSharers) pattern |= 1u << i;
+      mine &= pattern << from;
+    }
+    for (uint32_t left = mine; left; left &= left - 1) {
+      const int at = l * kChunk + lane + 32 * (__ffs(left) - 1), in_chunk = at + base - chunk_start;
+      if (kVary && (in_chunk < 0 || in_chunk >= kChunk)) continue;
+      x[in_chunk] = from_float<T>(changed(to_float(x[in_chunk]), at, r));
+    }
+  };
+  auto sharers_sync = [](int barrier) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(32 * kSharers) : "memory"); };
+  auto landed = [&](int w, int r) {
+    const uint32_t full = shared_address(&sh.full[w][r % kRing]), parity = (uint32_t)(r / kRing) & 1;
+    uint32_t ok = 0;
+    for (int i = 0; i < (1 << 22) && !ok; ++i)
+      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                   : "=r"(ok)
+                   : "r"(full), "r"(parity)
+                   : "memory");
+    return __all_sync(0xFFFFFFFFu, ok);
+  };
+  if (!streams) {
+    if (shared_chunk >= 0)
+      for (int r = 0; r < rows; ++r) {
+        sharers_sync(1);
+        landed(shared_chunk, r);  // (the copy's bytes are there: its own warp has seen it; this thread sees them by this)
+        change_listed(sh.ring[shared_chunk][r % kRing], s0 - lead_of(r) + shared_chunk * kChunk, shared_chunk, 1 + warp - kLogitWarps, kSharers, r);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        sharers_sync(2);
+      }
+    return;
+  }
+  for (int r = 0; r < rows; ++r) {
     const Piece c = kVary ? piece_of(r) : first;
     T* x = sh.ring[warp][r % kRing];
-    {
-      const uint32_t full = shared_address(&sh.full[warp][r % kRing]), parity = (uint32_t)(r / kRing) & 1;
-      uint32_t ok = 0;
-      for (int i = 0; i < (1 << 22) && !ok; ++i)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok)
-                     : "r"(full), "r"(parity)
-                     : "memory");
-      // (a copy that never lands: seen by whoever reads the row)
-      if (!__all_sync(0xFFFFFFFFu, ok)) {
-        for (int i = lane; i < kChunk; i += 32) x[i] = from_float<T>(__uint_as_float(0x7FC00000u));
-      }
+    // (a copy that never lands: seen by whoever reads the row)
+    if (!landed(warp, r)) {
+      for (int i = lane; i < kChunk; i += 32) x[i] = from_float<T>(__uint_as_float(0x7FC00000u));
     }
     __syncwarp();
     // ---- the listed tokens
     if (changes) {
-      for (int l = warp; l <= warp + (kVary ? 1 : 0); ++l) {
-        for (uint32_t left = kVary ? sh.touched[l][lane] : my_touched; left; left &= left - 1) {
-          const int at = l * kChunk + lane + 32 * (__ffs(left) - 1), in_chunk = at + base - c.start;
-          if (kVary && (in_chunk < 0 || in_chunk >= kChunk)) continue;
-          x[in_chunk] = from_float<T>(changed(to_float(x[in_chunk]), at, r));
-        }
-      }
+      if (warp == shared_chunk) sharers_sync(1);
+      change_listed(x, c.start, warp, 0, warp == shared_chunk ? kSharers : 1, r);
+      if (kVary) change_listed(x, c.start, warp + 1, 0, 1, r);
+      if (warp == shared_chunk) sharers_sync(2);
       __syncwarp();
     }
     const uint32_t bits = bits_of(r);
@@ -349,7 +392,7 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     }
     // ---- the next row to ask for takes the place of the one before this, which has been taken away meanwhile
     ask_mask(r + kMaskRing - 1);
-    if (r + kRing - 1 < p.R) {
+    if (r + kRing - 1 < rows) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kMaskRing - kRing) : "memory");
       if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
       __syncwarp();
@@ -437,9 +480,12 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return cuda_fail(e);
-  note_launch("process_logits_kernel<%s>: %d threads x (%d, %u) blocks", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads, B, slices);
+  // Blocks share the rows while there are fewer than two to an SM (each counts the slice's history for itself).
+  unsigned shares = 1;
+  while ((int64_t)B * slices * shares * 2 <= 2 * sm_count() && (int)shares * 4 <= R) shares *= 2;
+  note_launch("process_logits_kernel<%s>: %d threads x (%d, %u, %u) blocks", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads, B, slices, shares);
   // (all sequences' first slices before the next: frequent tokens have low numbers, their blocks the most to change)
-  Launch l(dim3((unsigned)B, slices, 1), kLogitThreads, smem, (cudaStream_t)cuda_stream);
+  Launch l(dim3((unsigned)B, slices, shares), kLogitThreads, smem, (cudaStream_t)cuda_stream);
   e = cudaLaunchKernelEx(&l.cfg, kernel, p);
   return e == cudaSuccess ? ERSD_OK : cuda_fail(e);
 }
