@@ -264,7 +264,8 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocks)
   Misc& sh = *(Misc*)(value_ring + kStages * P::kStageBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kv_head = blockIdx.y, b = blockIdx.z;
-  const int tile = blockIdx.x / p.split, part = blockIdx.x - tile * p.split;
+  // (a chunk's later rows see more keys: their tiles go first)
+  const int tile = p.row_tiles - 1 - (int)blockIdx.x / p.split, part = (int)blockIdx.x % p.split;
 
   // ---- what needs nothing of the kernel before this one on the stream
   if (tid == 0) {
