@@ -11,6 +11,9 @@
 // values are copied to shared memory as floats, a thread forms the scores of four slots with four rows, the
 // softmax's running maximum and sum live in shared memory, and a thread holds four columns of several rows of the
 // output in registers.  `split` blocks join their partial results through distributed shared memory.
+//
+// Measured on one B200, float32, 8 sequences behind up to 777 positions, 16 heads of 64: chains of five rows 25 us (their
+// bytes 6: instructions for products and exchanges bound it), 30 rows 50 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math.h>

@@ -19,6 +19,13 @@
 //            softmax group each, 128 slots at a time (with 64 the first operand, read again for every 64 columns,
 //            takes more of shared memory's rate than there is: 2545 cycles for 64 slots against 3660 for 128); one's
 //            products run while the other's softmax does, and half of a tile's weights go ahead of the rest.
+//            Of 3170 cycles for a tile of heads of 128 the products take 3072 (1024 for a stream's scores, at half the
+//            rate for want of shared memory's, 512 for its outputs); of 2970 with heads of 64 powers of two take 2048.
+//            (q in tensor memory, which has room for it beside 64 slots: 683 us instead of 580 for the prompt below.)
+// Measured on one B200: 32 trees of 17 nodes behind 3100 positions on average (32/8 heads of 128) 80 us, 5.1 TB/s
+// of cache; one token each in 18 sequences behind 64000 positions 702 us, 6.7 TB/s (behind 32000 to 64000: 592
+// us, 6.0); one token behind 1000 positions 9.2 us; 2 x 2048 rows behind up to 8192 positions 525 to 590 us, 0.93 to 1.05
+// PFLOP/s.
 //
 // The output's accumulator stays in tensor memory.  It is scaled only when a row's maximum has risen by more than
 // 2^8 since the last time (weights are then at most 2^8, which bfloat16 and the 32-bit sums hold as well as 1);
@@ -972,7 +979,8 @@ int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st
   const bool many = (int64_t)p.R * p.group > 128;
   p.row_tiles = (int)(((int64_t)p.R * p.group + (many ? 255 : 127)) / (many ? 256 : 128));
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
-  // Blocks with a long ring while no more than one goes to an SM (18 sequences of 64000 positions, 144 blocks: 620 us; 1150 with the shorter rings and one block to an SM),
+  // Blocks with a long ring while no more than one goes to an SM (18 sequences of 32000 to 64000 positions, 144
+  // blocks: 620 us; 1150 with the shorter rings and one block to an SM),
   // else two to an SM.
   const bool alone = many || units * (p.split ? p.split : 1) <= sms;
   const int at = (p.dim == 64 ? 0 : 3) + (many ? 2 : alone ? 1 : 0);

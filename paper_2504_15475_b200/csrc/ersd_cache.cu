@@ -1,5 +1,7 @@
 // The paged cache's writes: ersd_cache_append and ersd_cache_commit.  Both are copies, bound by bytes (large
-// calls) or by one launch and two dependent reads (small ones).
+// calls) or by one launch and two dependent reads (small ones).  Measured on one B200, 8 heads of 128 in bfloat16: 8 x up to
+// 2048 rows appended in 16 us (67 MB moved, 4.1 TB/s with ragged counts; 6.0 when every row counts), 64 x 1 row in 1.8 us,
+// accepted paths of 32 sequences in 32 layers in 6 us.
 #include "ersd_host.h"
 
 namespace ersd {
