@@ -9,11 +9,13 @@
 // chunk away.  A chunk of which the mask allows nothing is not read.
 //
 // Measured on one B200, bfloat16: 64 chains of nine rows x 128256 tokens behind up to 4096 tokens, all penalties and 64 biases,
-// 67 to 72 us (4.1 to 4.4 TB/s; without any change 48 us: instructions for the slices of the frequent tokens are the rest); 32
-// trees of 17 rows x 151936 under masks 81 to 86 us (68 without penalties); one float32 row of 32000 in 3.7 us.
-// Counts of 4096 tokens by each block that shares a sequence's rows are what a small batch costs: one such chain 10.9 us.
+// 67 us (4.4 TB/s; without any change 48 us: instructions for the slices of the frequent tokens are the rest); 32
+// trees of 17 rows x 151936 under masks 81 us (68 without penalties); one float32 row of 32000 in 4.1 us.
+// Counts of 4096 tokens by each block that shares a sequence's rows are what a small batch costs: one such chain 10.8 us.
 #include <cuda_bf16.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "ersd_host.h"
 
@@ -31,6 +33,7 @@ constexpr int kLead = 8;              // most tokens a row's chunks start before
 constexpr int kSpan = kSlice + kLead;
 constexpr int kLists = kLogitWarps + 1;
 constexpr int kMany = 64;             // tokens with an entry from which on a chunk is shared, see below
+constexpr int kFewBlocks = 8;         // to an SM, of which up to four run at a time: up to here kFew, see below
 constexpr int kSharers = 1 + kLogitWarps;  // its own warp and those that have none
 // An entry of the table: how often the token occurs behind the prompt, and
 constexpr uint32_t kSeen = 1u << 31;     // that it is in the history
@@ -109,7 +112,10 @@ constexpr size_t kBiasBytes = sizeof(uint32_t) * kSpan, kMaskBytes = sizeof(uint
 
 // kVary: rows of the input start at different distances from a 16-byte boundary (else what a warp's chunk is, is
 // worked out once and not for every row).
-template <typename T, bool kVary>
+// kFew: few blocks, so that a block's own time counts: several may share a sequence's rows, and a block's warps the
+// chunk with the most to change.  With many blocks others fill what a waiting block leaves, and only what this takes
+// by itself would show (64 chains of nine rows, 2048 blocks: 71.5 us instead of 67; 32 chains 39 instead of 43).
+template <typename T, bool kVary, bool kFew>
 __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __grid_constant__ LogitParams p) {
   extern __shared__ __align__(128) char raw[];
   LogitShared<T>& sh = *(LogitShared<T>*)raw;
@@ -118,8 +124,9 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   constexpr int kPer16 = 16 / (int)sizeof(T);
   const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int s0 = (int)blockIdx.y * kSlice;
-  // with few sequences several blocks share the rows: this one has `rows` of them from row0 on, which it counts from 0
-  const int row0 = (int)((int64_t)p.R * blockIdx.z / gridDim.z), rows = (int)((int64_t)p.R * (blockIdx.z + 1) / gridDim.z) - row0;
+  // with few sequences several blocks may share the rows: this one has `rows` of them from row0 on, which it counts from 0
+  const int row0 = kFew ? (int)((int64_t)p.R * blockIdx.z / gridDim.z) : 0;
+  const int rows = kFew ? (int)((int64_t)p.R * (blockIdx.z + 1) / gridDim.z) - row0 : p.R;
   // Chunks start on 16-byte boundaries of the input, `lead` tokens before the slice's own start.  Where all rows
   // have the same lead the table starts there, and a warp's chunk is a chunk of the table; else it starts kLead
   // before, and a warp's chunk of a row lies in two chunks of the table.
@@ -307,7 +314,8 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   // without a chunk take their share in every row, or its own warp would hold up the block (4 us for each row with
   // histories of 3000 tokens).
   int shared_chunk = -1;
-  if (changes) {
+  // (not looked for where rows times tokens are few: 4.05 us instead of 4.25 for a row with 208 tokens)
+  if (kFew && (int64_t)rows * (p.history_width + p.bias_count) >= 4 * kMany) {
     if (warp < kLogitWarps) {
       const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(sh.touched[warp][lane]));
       if (lane == 0) sh.listed[warp] = n;
@@ -345,7 +353,7 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     return __all_sync(0xFFFFFFFFu, ok);
   };
   if (!streams) {
-    if (shared_chunk >= 0)
+    if (kFew && shared_chunk >= 0)
       for (int r = 0; r < rows; ++r) {
         sharers_sync(1);
         landed(shared_chunk, r);  // (the copy's bytes are there: its own warp has seen it; this thread sees them by this)
@@ -365,10 +373,10 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
     __syncwarp();
     // ---- the listed tokens
     if (changes) {
-      if (warp == shared_chunk) sharers_sync(1);
-      change_listed(x, c.start, warp, 0, warp == shared_chunk ? kSharers : 1, r);
+      if (kFew && warp == shared_chunk) sharers_sync(1);
+      change_listed(x, c.start, warp, 0, kFew && warp == shared_chunk ? kSharers : 1, r);
       if (kVary) change_listed(x, c.start, warp + 1, 0, 1, r);
-      if (warp == shared_chunk) sharers_sync(2);
+      if (kFew && warp == shared_chunk) sharers_sync(2);
       __syncwarp();
     }
     const uint32_t bits = bits_of(r);
@@ -480,14 +488,19 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
   p.long_history = o.history && o.history_width > (int)kShortCount;
   const bool lead = vary || !aligned_to(logits, 16);
   smem += (p.bias_count && p.long_history ? kBiasBytes : 0) + (p.mask ? (lead ? 2 : 1) * kMaskBytes : 0);
-  const auto kernel = dt == ERSD_BF16 ? (vary ? process_logits_kernel<__nv_bfloat16, true> : process_logits_kernel<__nv_bfloat16, false>)
-                                      : (vary ? process_logits_kernel<float, true> : process_logits_kernel<float, false>);
+  const bool few = (int64_t)B * slices <= kFewBlocks * sm_count();
+  const auto build = [&](auto is_few) {
+    constexpr bool kFew = decltype(is_few)::value;
+    return dt == ERSD_BF16 ? (vary ? process_logits_kernel<__nv_bfloat16, true, kFew> : process_logits_kernel<__nv_bfloat16, false, kFew>)
+                           : (vary ? process_logits_kernel<float, true, kFew> : process_logits_kernel<float, false, kFew>);
+  };
+  const auto kernel = few ? build(std::true_type()) : build(std::false_type());
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return cuda_fail(e);
   // Blocks share the rows while there are fewer than two to an SM (each counts the slice's history for itself).
   unsigned shares = 1;
-  while ((int64_t)B * slices * shares * 2 <= 2 * sm_count() && (int)shares * 4 <= R) shares *= 2;
+  while (few && (int64_t)B * slices * shares * 2 <= 2 * sm_count() && (int)shares * 4 <= R) shares *= 2;
   note_launch("process_logits_kernel<%s>: %d threads x (%d, %u, %u) blocks", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads, B, slices, shares);
   // (all sequences' first slices before the next: frequent tokens have low numbers, their blocks the most to change)
   Launch l(dim3((unsigned)B, slices, shares), kLogitThreads, smem, (cudaStream_t)cuda_stream);

@@ -153,6 +153,35 @@ def test_padded_rows_and_boundaries(ersd, dtype):
             assert (dst[..., :out_lead] == 5.0).all() and (dst[..., out_lead + 500:] == 5.0).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [6000, 6001])
+@pytest.mark.parametrize("mask", [False, True])
+def test_frequent_tokens(ersd, dtype, V, mask):
+    """Long histories whose tokens lie close together, rows that several blocks share."""
+    for parent, B, R, history in ((None, 2, 9, 2000), (list(wl.TREE_4x4), 1, len(wl.TREE_4x4), 9000), (None, 3, 1, 700)):
+        x, a = make(B, R, V, dtype, parent=parent, history=history, biases=90, seed=12)
+        a["history_lens"] = None
+        if not mask:
+            a["mask"] = None
+            x = torch.nan_to_num(x, nan=1.0)
+        check(ersd, x, a)
+        if mask:
+            check(ersd, x, a, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 41])
+def test_many_sequences(ersd, dtype, V):
+    """More blocks than the device runs at a time."""
+    x, a = make(1300, 5, V, dtype, parent=[-1, 0, 0, 1, 1], history=70, seed=13)
+    check(ersd, x, a)
+    check(ersd, x, a, in_place=True)
+    a["mask"] = None
+    x = torch.nan_to_num(x, nan=1.0)
+    check(ersd, x, a)
+    check(ersd, x, a, in_place=True)
+
+
 def test_the_same_call_again_and_captured(ersd):
     x, a = make(4, 9, 32000, torch.bfloat16, history=3000, seed=10)
     dev = {k: t.cuda() if torch.is_tensor(t) else t for k, t in a.items()}
