@@ -19,7 +19,7 @@
 //            softmax group each, 128 slots at a time (with 64 the first operand, read again for every 64 columns,
 //            takes more of shared memory's rate than there is: 2545 cycles for 64 slots against 3660 for 128); one's
 //            products run while the other's softmax does, and half of a tile's weights go ahead of the rest.
-//            Of 3170 cycles for a tile of heads of 128 the products take 3072 (1024 for a stream's scores, at half the
+//            Of 3170 cycles for a tile of heads of 128 the products take 97 % (1024 for a stream's scores, at half the
 //            rate for want of shared memory's, 512 for its outputs); of 2970 with heads of 64 powers of two take 2048.
 //            (q in tensor memory, which has room for it beside 64 slots: 683 us instead of 580 for the prompt below.)
 // Measured on one B200: 32 trees of 17 nodes behind 3100 positions on average (32/8 heads of 128) 80 us, 5.1 TB/s
