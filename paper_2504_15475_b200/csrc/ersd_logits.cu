@@ -314,8 +314,9 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   // without a chunk take their share in every row, or its own warp would hold up the block (4 us for each row with
   // histories of 3000 tokens).
   int shared_chunk = -1;
-  // (not looked for where rows times tokens are few: 4.05 us instead of 4.25 for a row with 208 tokens)
-  if (kFew && (int64_t)rows * (p.history_width + p.bias_count) >= 4 * kMany) {
+  // (not looked for where rows times tokens are few: 4.05 us instead of 4.25 for a row with 208 tokens; without `changes`
+  // there are no lists, and no changes of the chunk's own warp for the others to meet it at)
+  if (kFew && changes && (int64_t)rows * (p.history_width + p.bias_count) >= 4 * kMany) {
     if (warp < kLogitWarps) {
       const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(sh.touched[warp][lane]));
       if (lane == 0) sh.listed[warp] = n;
@@ -451,7 +452,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
                          o.bias_values, o.mask};
   for (const void* w : words)
     if (!aligned_to(w, 4)) return ERSD_EALIGN;
-  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || o.history_width > (1 << 30) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
+  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || (o.history && o.history_width > (1 << 30)) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
   if (o.draft_tokens && o.parent && !is_tree(o.parent, R)) return ERSD_EINVAL;
   LogitParams p;
   memset(&p, 0, sizeof p);
@@ -467,7 +468,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
   p.history = o.history;
   p.history_lens = o.history_lens;
   p.prompt_lens = o.prompt_lens;
-  p.history_width = o.history_width;
+  p.history_width = o.history ? o.history_width : 0;  // (a width alone plays no part)
   p.draft_tokens = R > 1 ? o.draft_tokens : nullptr;
   p.tree = o.draft_tokens && o.parent;
   if (p.tree)
