@@ -452,7 +452,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
                          o.bias_values, o.mask};
   for (const void* w : words)
     if (!aligned_to(w, 4)) return ERSD_EALIGN;
-  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || (o.history && o.history_width > (1 << 30)) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
+  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || (o.history && o.history_width > (int)kLongCount) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
   if (o.draft_tokens && o.parent && !is_tree(o.parent, R)) return ERSD_EINVAL;
   LogitParams p;
   memset(&p, 0, sizeof p);

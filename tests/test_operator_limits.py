@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_operator_refusals import EINVAL, LogitOpts, P, opts, ptr
+from test_operator_refusals import EINVAL, EUNSUP, LogitOpts, P, opts, ptr
 
 from paper_2504_15475_b200 import build as ersd_build
 
@@ -28,3 +28,10 @@ def test_a_width_without_a_history_is_left_out(L):
     tree = dict(draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p))
     for width in (0, 4096, 1 << 30, 0x7FFFFFFF):
         assert logits(L, history_width=width, **tree) == EINVAL, width
+
+
+def test_histories_beyond_a_count(L):
+    """Counts of a token have 29 bits."""
+    for width in (1 << 29, (1 << 29) + 1, 1 << 30, 0x7FFFFFFF):
+        assert logits(L, history=P, history_width=width, draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p)) == EUNSUP, width
+    assert logits(L, history=P, history_width=(1 << 29) - 1, draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p)) == EINVAL
