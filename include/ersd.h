@@ -487,7 +487,7 @@ typedef struct ersd_logit_opts {
  * Entries V..ld-1 of a row are left alone.
  * Errors: ERSD_EINVAL (null pointers, sizes < 1, strides below V, draft_tokens or parent that do not
  * go with R, values without tokens, ...); ERSD_EALIGN; ERSD_EUNSUPPORTED for B or R > 65535, draft
- * tokens with R > ERSD_MAX_ROWS, V > 2^28, history_width >= 2^29, bias_count > ERSD_MAX_BIASES.
+ * tokens with R > ERSD_MAX_ROWS, V > 268431353 (65535 blocks of 4096, less 7), history_width >= 2^29, bias_count > ERSD_MAX_BIASES.
  */
 int ersd_process_logits(const void* logits, void* out, ersd_dtype dt, int B, int R, int V, const ersd_logit_opts* opts,
                         void* cuda_stream);

@@ -33,6 +33,7 @@ constexpr int kLead = 8;              // most tokens a row's chunks start before
 constexpr int kSpan = kSlice + kLead;
 constexpr int kLists = kLogitWarps + 1;
 constexpr int kMany = 64;             // tokens with an entry from which on a chunk is shared, see below
+constexpr int kMaxVocab = 65535 * kSlice - (kLead - 1);  // a grid has 65535 slices
 constexpr int kFewBlocks = 8;         // to an SM, of which up to four run at a time: up to here kFew, see below
 constexpr int kSharers = 1 + kLogitWarps;  // its own warp and those that have none
 // An entry of the table: how often the token occurs behind the prompt, and
@@ -452,7 +453,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
                          o.bias_values, o.mask};
   for (const void* w : words)
     if (!aligned_to(w, 4)) return ERSD_EALIGN;
-  if (B > 65535 || R > 65535 || V > (1 << 28) || o.bias_count > ERSD_MAX_BIASES || (o.history && o.history_width > (int)kLongCount) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
+  if (B > 65535 || R > 65535 || V > kMaxVocab || o.bias_count > ERSD_MAX_BIASES || (o.history && o.history_width > (int)kLongCount) || (o.draft_tokens && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
   if (o.draft_tokens && o.parent && !is_tree(o.parent, R)) return ERSD_EINVAL;
   LogitParams p;
   memset(&p, 0, sizeof p);

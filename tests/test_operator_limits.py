@@ -35,3 +35,12 @@ def test_histories_beyond_a_count(L):
     for width in (1 << 29, (1 << 29) + 1, 1 << 30, 0x7FFFFFFF):
         assert logits(L, history=P, history_width=width, draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p)) == EUNSUP, width
     assert logits(L, history=P, history_width=(1 << 29) - 1, draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p)) == EINVAL
+
+
+def test_vocabularies_beyond_the_grid(L):
+    """A slice of 4096 tokens to a block, 65535 blocks along the vocabulary."""
+    tree = dict(draft_tokens=P, parent=C.cast(BAD_TREE, C.c_void_p))
+    most = 65535 * 4096 - 7
+    for V in (most + 1, 1 << 28):
+        assert logits(L, V=V, **tree) == EUNSUP, V
+    assert logits(L, V=most, **tree) == EINVAL
