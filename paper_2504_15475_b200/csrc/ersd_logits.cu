@@ -15,6 +15,7 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <mutex>
 #include <type_traits>
 
 #include "ersd_host.h"
@@ -433,6 +434,23 @@ __global__ void __launch_bounds__(kLogitThreads) process_logits_kernel(const __g
   if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // (shared memory goes with the block)
 }
 
+// What a build (one of eight) needs before its first launch on a device: room for the call that needs the most shared
+// memory.  (Set to a call's own need it would change under another thread's launch.)
+int prepare_build(const void* kernel, int at, size_t most) {
+  static std::mutex m;
+  static uint64_t ready[8];  // a bit for each device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e);
+  if (dev < 0 || dev >= 64) return ERSD_EUNSUPPORTED;
+  std::lock_guard<std::mutex> lock(m);
+  if (ready[at] >> dev & 1) return ERSD_OK;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  if (e != cudaSuccess) return cuda_fail(e);
+  ready[at] |= (uint64_t)1 << dev;
+  return ERSD_OK;
+}
+
 }  // namespace
 
 }  // namespace ersd
@@ -489,6 +507,7 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
   size_t smem = dt == ERSD_BF16 ? sizeof(LogitShared<__nv_bfloat16>) : sizeof(LogitShared<float>);
   p.long_history = o.history && o.history_width > (int)kShortCount;
   const bool lead = vary || !aligned_to(logits, 16);
+  const size_t most = smem + kBiasBytes + 2 * kMaskBytes;
   smem += (p.bias_count && p.long_history ? kBiasBytes : 0) + (p.mask ? (lead ? 2 : 1) * kMaskBytes : 0);
   const bool few = (int64_t)B * slices <= kFewBlocks * sm_count();
   const auto build = [&](auto is_few) {
@@ -497,15 +516,14 @@ extern "C" int ersd_process_logits(const void* logits, void* out, ersd_dtype dt,
                            : (vary ? process_logits_kernel<float, true, kFew> : process_logits_kernel<float, false, kFew>);
   };
   const auto kernel = few ? build(std::true_type()) : build(std::false_type());
-  cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return cuda_fail(e);
+  const int status = prepare_build((const void*)kernel, (dt == ERSD_BF16 ? 4 : 0) + (vary ? 2 : 0) + (few ? 1 : 0), most);
+  if (status != ERSD_OK) return status;
   // Blocks share the rows while there are fewer than two to an SM (each counts the slice's history for itself).
   unsigned shares = 1;
   while (few && (int64_t)B * slices * shares * 2 <= 2 * sm_count() && (int)shares * 4 <= R) shares *= 2;
   note_launch("process_logits_kernel<%s>: %d threads x (%d, %u, %u) blocks", dt == ERSD_BF16 ? "bf16" : "f32", kLogitThreads, B, slices, shares);
   // (all sequences' first slices before the next: frequent tokens have low numbers, their blocks the most to change)
   Launch l(dim3((unsigned)B, slices, shares), kLogitThreads, smem, (cudaStream_t)cuda_stream);
-  e = cudaLaunchKernelEx(&l.cfg, kernel, p);
+  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, kernel, p);
   return e == cudaSuccess ? ERSD_OK : cuda_fail(e);
 }
