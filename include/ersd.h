@@ -435,7 +435,8 @@ int ersd_cache_append(const ersd_cache* cache, const void* k_new, const void* v_
  * of node path[b, j] move from slot context_lens[b] + path[b, j] to slot context_lens[b] + j.
  *   path device [B, D+1] int32: opts->out_path of the verification (ascending, from node 0)
  *   accept_len device [B] int32; accept_len < 0 moves nothing
- *   out_context_lens device [B] int32, nullable, not context_lens itself: context_lens[b] + accept_len[b] + 1
+ *   out_context_lens device [B] int32, nullable: context_lens[b] + accept_len[b] + 1.  Memory of its own: ERSD_EINVAL
+ *     where it meets context_lens, path or accept_len
  * Errors as above.
  */
 int ersd_cache_commit(const ersd_cache* cache, const int32_t* context_lens, const int32_t* path, const int32_t* accept_len, int B,

@@ -137,6 +137,12 @@ bool pieces_of_16(const Side& s, int64_t row_bytes) {
   return (all & 15) == 0 && aligned_to(s.cache, 16) && aligned_to(s.rows, 16);
 }
 
+// Whether n numbers from a on and m from b on have any in common.
+bool meet(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + 4 * (uintptr_t)m && y < x + 4 * (uintptr_t)n;
+}
+
 }  // namespace
 
 }  // namespace ersd
@@ -186,8 +192,12 @@ extern "C" int ersd_cache_commit(const ersd_cache* cache, const int32_t* context
   CacheParams p;
   const int st = read_cache(cache, &c, &p);
   if (st != ERSD_OK) return st;
-  if (!context_lens || !path || !accept_len || B < 1 || D < 0 || out_context_lens == context_lens) return ERSD_EINVAL;
+  if (!context_lens || !path || !accept_len || B < 1 || D < 0) return ERSD_EINVAL;
   if (!aligned_to(context_lens, 4) || !aligned_to(path, 4) || !aligned_to(accept_len, 4) || !aligned_to(out_context_lens, 4)) return ERSD_EALIGN;
+  // (a sequence's other blocks may still have to read what its first would write over)
+  if (out_context_lens && (meet(out_context_lens, B, context_lens, B) || meet(out_context_lens, B, accept_len, B) ||
+                           meet(out_context_lens, B, path, (int64_t)B * ((int64_t)D + 1))))
+    return ERSD_EINVAL;
   if (B > 65535 || D >= ERSD_MAX_ROWS || c.layers > (1 << 20)) return ERSD_EUNSUPPORTED;
   const int64_t size = c.dtype == ERSD_BF16 ? 2 : 4, d = c.head_dim;
   p.context_lens = context_lens;

@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_operator_refusals import EINVAL, EUNSUP, LogitOpts, P, opts, ptr
+from test_operator_refusals import EINVAL, EUNSUP, LogitOpts, P, cache, opts, ptr
 
 from paper_2504_15475_b200 import build as ersd_build
 
@@ -44,3 +44,16 @@ def test_vocabularies_beyond_the_grid(L):
     for V in (most + 1, 1 << 28):
         assert logits(L, V=V, **tree) == EUNSUP, V
     assert logits(L, V=most, **tree) == EINVAL
+
+
+def test_lengths_written_over_what_the_commit_reads(L):
+    """Blocks of one sequence read lengths, paths and counts while another writes the new lengths."""
+    def commit(out, lens=0x10000, path=0x20000, accept=0x30000, B=4, D=3):
+        # (the path's alignment is right, and the cache has a size that is refused last)
+        return L.ersd_cache_commit(ptr(cache(layers=(1 << 20) + 1)), ptr(lens), ptr(path), ptr(accept), B, D, ptr(out), None)
+
+    for base, size in ((0x10000, 16), (0x20000, 64), (0x30000, 16)):
+        for out in (base, base + 4, base + size - 4, base - 12):
+            assert commit(out) == EINVAL, hex(out)
+        for out in (base - 16, base + size):
+            assert commit(out) == EUNSUP, hex(out)
