@@ -359,6 +359,7 @@ int ersd_acceptance_profile(const int32_t* paths, const int32_t* parent, int B, 
  * Slots beyond max_pages * page_size do not exist, and a page outside [0, num_pages) is never
  * touched: rows for them are not written, and as keys the slots of such a page count as zeros.
  * Lengths below 0 count as 0 (in ersd_chunk_attention those beyond 2^30 - 1 as that).  Strides are in elements; the innermost dimension is contiguous.
+ * Where rows are written, a stride of 0 between several of them is refused (ERSD_EINVAL).
  * These calls need no workspace, allocate nothing and can be captured.
  */
 typedef struct ersd_cache {

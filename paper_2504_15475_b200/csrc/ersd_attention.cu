@@ -616,10 +616,11 @@ extern "C" int ersd_chunk_attention(const ersd_cache* cache, const void* q, void
   if (c.head_dim > ERSD_MAX_HEAD_DIM || B > 65535 || c.heads > 65535 || (o.parent && R > ERSD_MAX_ROWS)) return ERSD_EUNSUPPORTED;
   if ((int64_t)R * Hq > (1 << 30) || (int64_t)c.max_pages * c.page_size > (1 << 30)) return ERSD_EUNSUPPORTED;
   if (o.parent && !is_tree(o.parent, R)) return ERSD_EINVAL;
+  const bool qs = o.a_stride_b || o.a_stride_r || o.a_stride_h, os = o.b_stride_b || o.b_stride_r || o.b_stride_h;
+  if (os && ((B > 1 && !o.b_stride_b) || (R > 1 && !o.b_stride_r) || (Hq > 1 && !o.b_stride_h))) return ERSD_EINVAL;  // (rows written over one another)
   AttentionParams p;
   memset(&p, 0, sizeof p);
   const int64_t d = c.head_dim;
-  const bool qs = o.a_stride_b || o.a_stride_r || o.a_stride_h, os = o.b_stride_b || o.b_stride_r || o.b_stride_h;
   p.q = q;
   p.k = c.k;
   p.v = c.v;

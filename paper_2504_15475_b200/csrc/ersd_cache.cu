@@ -137,6 +137,11 @@ bool pieces_of_16(const Side& s, int64_t row_bytes) {
   return (all & 15) == 0 && aligned_to(s.cache, 16) && aligned_to(s.rows, 16);
 }
 
+// Whether two rows of a side that is written lie in the same place for want of a stride.
+bool shares_rows(const ersd_cache& c, const Side& s) {
+  return (c.heads > 1 && !s.head) || (c.page_size > 1 && !s.token) || (c.num_pages > 1 && !s.page);
+}
+
 // Whether n numbers from a on and m from b on have any in common.
 bool meet(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -169,6 +174,7 @@ extern "C" int ersd_cache_append(const ersd_cache* cache, const void* k_new, con
   p.side[1].row_b = (vb ? o.b_stride_b : R * c.heads * d) * size;
   p.side[1].row_r = (vb ? o.b_stride_r : c.heads * d) * size;
   p.side[1].row_h = (vb ? o.b_stride_h : d) * size;
+  if (shares_rows(c, p.side[0]) || shares_rows(c, p.side[1])) return ERSD_EINVAL;
   p.context_lens = context_lens;
   p.row_counts = o.row_counts;
   p.B = B;
@@ -199,6 +205,7 @@ extern "C" int ersd_cache_commit(const ersd_cache* cache, const int32_t* context
                            meet(out_context_lens, B, path, (int64_t)B * ((int64_t)D + 1))))
     return ERSD_EINVAL;
   if (B > 65535 || D >= ERSD_MAX_ROWS || c.layers > (1 << 20)) return ERSD_EUNSUPPORTED;
+  if (shares_rows(c, p.side[0]) || shares_rows(c, p.side[1]) || (c.layers > 1 && (!p.side[0].layer || !p.side[1].layer))) return ERSD_EINVAL;
   const int64_t size = c.dtype == ERSD_BF16 ? 2 : 4, d = c.head_dim;
   p.context_lens = context_lens;
   p.path = path;

@@ -31,3 +31,30 @@ def test_largest_vocabulary(ersd, dtype):
     with pytest.raises(ersd.ErsdError) as e:
         ersd.ersd_process_logits(*[torch.zeros(1, 1, V + 1, dtype=dtype, device="cuda")] * 2)
     assert e.value.status == -3
+
+
+def test_expanded_tensors_are_read_but_not_written(ersd):
+    """Queries of one row, keys of one head: expanded ones are as good as copies.  Outputs and caches that are written: refused."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for dtype in (torch.float32, torch.bfloat16):
+        q = torch.randn(2, 1, 4, 64, generator=gen, device="cuda").to(dtype).expand(2, 3, 4, 64)
+        k, v = (torch.randn(4, 16, 1, 64, generator=gen, device="cuda").to(dtype).expand(4, 16, 2, 64) for _ in range(2))
+        table = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+        lens = torch.tensor([20, 7], dtype=torch.int32, device="cuda")
+        out, want = torch.empty(2, 2, 3, 4, 64, dtype=dtype, device="cuda")
+        ersd.ersd_chunk_attention(q, k, v, table, lens, out, kernel_path=1)
+        ersd.ersd_chunk_attention(q.contiguous(), k.contiguous(), v.contiguous(), table, lens, want, kernel_path=1)
+        assert torch.equal(out, want)
+        ersd.ersd_chunk_attention(q, k, v, table, lens, out)                # (heads in one place: not for tensor cores)
+        assert torch.equal(out, want)
+        one = torch.zeros(2, 3, 2, 64, dtype=dtype, device="cuda")
+        path, accept = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+        whole = k.contiguous()
+        for call in (lambda: ersd.ersd_chunk_attention(q, k, v, table, lens, out[:, :1].expand(2, 3, 4, 64)),
+                     lambda: ersd.ersd_cache_append(one, one, whole, v, table, lens),
+                     lambda: ersd.ersd_cache_append(one, one, k, whole, table, lens),
+                     lambda: ersd.ersd_cache_commit(whole, v, table, lens, path, accept),
+                     lambda: ersd.ersd_cache_commit(whole.expand(3, *whole.shape), whole.expand(3, *whole.shape), table, lens, path, accept)):
+            with pytest.raises(ersd.ErsdError) as e:
+                call()
+            assert e.value.status == -1

@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_operator_refusals import EINVAL, EUNSUP, LogitOpts, P, cache, opts, ptr
+from test_operator_refusals import ChunkOpts, EINVAL, EUNSUP, LogitOpts, P, cache, opts, ptr
 
 from paper_2504_15475_b200 import build as ersd_build
 
@@ -57,3 +57,17 @@ def test_lengths_written_over_what_the_commit_reads(L):
             assert commit(out) == EINVAL, hex(out)
         for out in (base - 16, base + size):
             assert commit(out) == EUNSUP, hex(out)
+
+
+def test_memory_that_several_rows_would_share(L):
+    """Strides of 0 where rows are written: an expanded tensor is no place for outputs or a cache's writes."""
+    f32 = dict(dtype=0)
+    bad = [dict(k_stride_head=0), dict(v_stride_head=0), dict(k_stride_token=0), dict(v_stride_token=0), dict(k_stride_page=0),
+           dict(v_stride_page=0)]
+    for kw in bad:
+        assert L.ersd_cache_append(ptr(cache(**kw)), ptr(P), ptr(P), ptr(P), 1, 3, None, None) == EINVAL, kw
+        assert L.ersd_cache_commit(ptr(cache(**f32, **kw)), ptr(P), ptr(P), ptr(P), 1, 3, None, None) == EINVAL, kw
+    assert L.ersd_cache_commit(ptr(cache(layers=2, k_stride_layer=1 << 20)), ptr(P), ptr(P), ptr(P), 1, 3, None, None) == EINVAL
+    for b, r, h in ((0, 256, 64), (768, 0, 64), (768, 256, 0)):
+        o = opts(ChunkOpts, b_stride_b=b, b_stride_r=r, b_stride_h=h)
+        assert L.ersd_chunk_attention(ptr(cache()), ptr(P), ptr(P), ptr(P), 2, 3, 4, ptr(o), None) == EINVAL, (b, r, h)
