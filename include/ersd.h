@@ -414,7 +414,7 @@ typedef struct ersd_chunk_opts {
  * of 4, k and v on 16-byte boundaries in every stride run on tensor cores, with the softmax weights
  * rounded to bfloat16 for the second product; the rest on 32-bit arithmetic.
  * Errors: ERSD_EINVAL (null pointers, sizes < 1, Hq not a multiple of heads, window or sinks < 0, bad
- * parent, scale not finite); ERSD_EALIGN (a pointer off its element size); ERSD_EUNSUPPORTED for
+ * parent, scale not a number or beyond 2.3e38); ERSD_EALIGN (a pointer off its element size); ERSD_EUNSUPPORTED for
  * head_dim > ERSD_MAX_HEAD_DIM, a tree of more than ERSD_MAX_ROWS rows, B or heads > 65535, R * Hq or
  * max_pages * page_size beyond 2^30.
  */

@@ -608,7 +608,7 @@ extern "C" int ersd_chunk_attention(const ersd_cache* cache, const void* q, void
   if (!c.k || !c.v || !c.block_table || (c.dtype != ERSD_F32 && c.dtype != ERSD_BF16)) return ERSD_EINVAL;
   if (c.num_pages < 1 || c.page_size < 1 || c.heads < 1 || c.head_dim < 1 || c.layers < 1 || c.max_pages < 1) return ERSD_EINVAL;
   if (!q || !out || !context_lens || B < 1 || R < 1 || Hq < 1 || Hq % c.heads) return ERSD_EINVAL;
-  if (o.window < 0 || o.sinks < 0 || o.max_context < 0 || !(fabsf(o.scale) <= 3e38f) || o.kernel_path > 2) return ERSD_EINVAL;
+  if (o.window < 0 || o.sinks < 0 || o.max_context < 0 || !(fabsf(o.scale) <= 2.3e38f) || o.kernel_path > 2) return ERSD_EINVAL;
   if (o.split < 0 || o.split > 16) return ERSD_EINVAL;
   const size_t size = c.dtype == ERSD_BF16 ? 2 : 4;
   if (!aligned_to(c.k, size) || !aligned_to(c.v, size) || !aligned_to(q, size) || !aligned_to(out, size)) return ERSD_EALIGN;

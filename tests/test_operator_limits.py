@@ -71,3 +71,12 @@ def test_memory_that_several_rows_would_share(L):
     for b, r, h in ((0, 256, 64), (768, 0, 64), (768, 256, 0)):
         o = opts(ChunkOpts, b_stride_b=b, b_stride_r=r, b_stride_h=h)
         assert L.ersd_chunk_attention(ptr(cache()), ptr(P), ptr(P), ptr(P), 2, 3, 4, ptr(o), None) == EINVAL, (b, r, h)
+
+
+def test_scales_that_no_power_of_two_can_take(L):
+    """The softmax works with scale * log2(e), which has to be a number too."""
+    late = dict(parent=C.cast(BAD_TREE, C.c_void_p))  # refused last
+    for scale in (2.4e38, -2.4e38, 3e38, 3.4e38):
+        assert L.ersd_chunk_attention(ptr(cache()), ptr(P), ptr(P), ptr(P), 1, 300, 4, ptr(opts(ChunkOpts, scale=scale, **late)), None) == EINVAL, scale
+    for scale in (2.3e38, -2.3e38, 1e-45, 0.0):
+        assert L.ersd_chunk_attention(ptr(cache()), ptr(P), ptr(P), ptr(P), 1, 300, 4, ptr(opts(ChunkOpts, scale=scale, **late)), None) == EUNSUP, scale
