@@ -1,6 +1,6 @@
 // ersd_chunk_attention: checks, the choice of the kernel, and the kernels of 32-bit arithmetic.
 //
-// Up to 48 packed rows (see AttentionParams), where the cache's bytes bound the call: rows_kernel takes four.
+// Up to 48 packed rows (see AttentionParams and few_rows), where the cache's bytes are to bound the call: rows_kernel takes four.
 // L lanes share a slot, eight elements of its key and value in registers each, so that a warp has 32 / L slots at a
 // time and every warp goes through its own slots without waiting for another: the lanes' parts of the scores are
 // summed and dealt out by a few exchanges (lane r ends with row r's), lane r weighs row r's, and each lane adds its
@@ -544,7 +544,17 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) rows_kernel(const Attention
   cluster.sync();  // (no block ends while another reads its shared memory)
 }
 
-constexpr int kFewRows = 48;  // (30 rows: 50 us against 99 of tile_kernel, whose tiles are of 64 whether the rows are there or not)
+// Up to how many packed rows of a kv head rows_kernel takes, which goes through the cache once for every four, while
+// tile_kernel's tiles are of 64 whether the rows are there or not (rows_kernel / tile_kernel, us):
+//                                            36 rows        48 rows      bfloat16: 36 rows    48 rows
+//   8 x 777 positions, 16 heads of 64         72 / 91       103 / 91          93 / 93         136 / 94
+//   2 x 300, 8 heads of 64                    11 / 23        13 / 23          13 / 24          15 / 24
+//   32 x 3000, 8 heads of 64                 549 / 651      788 / 652        949 / 704       1359 / 701
+//   8 x 1500, 8 heads of 80                  159 / 166      310 / 169        193 / 183        368 / 184
+//   4 x 1500, 8 heads of 128                  69 / 131      125 / 133         87 / 142        166 / 144
+//   16 x 3000, 8 heads of 128                544 / 756      776 / 759        938 / 899       1375 / 900
+//   4 x 1500, 8 heads of 256                 141 / 276      277 / 286        167 / 250        325 / 254
+constexpr int few_rows(bool bf16) { return bf16 ? 36 : 48; }
 
 struct Build {
   const void* kernel;
@@ -560,14 +570,14 @@ Build rows_build(int dim) {
 }
 template <typename T>
 Build build_of(int64_t rows, int dim) {
-  if (rows <= kFewRows) return rows_build<T, kRows>(dim);
+  if (rows <= few_rows(sizeof(T) == 2)) return rows_build<T, kRows>(dim);
   if (dim <= 64) return {(const void*)tile_kernel<T, 64, 64>, sizeof(Shared<64, 64>), 64, kThreads, kNK};
   if (dim <= 128) return {(const void*)tile_kernel<T, 64, 128>, sizeof(Shared<64, 128>), 64, kThreads, kNK};
   return {(const void*)tile_kernel<T, 64, 256>, sizeof(Shared<64, 256>), 64, kThreads, kNK};
 }
 
 int launch_attention_f32(AttentionParams& p, bool bf16, int max_context, cudaStream_t st) {
-  const bool few = (int64_t)p.R * p.group <= kFewRows;
+  const bool few = (int64_t)p.R * p.group <= few_rows(bf16);
   const Build k = bf16 ? build_of<__nv_bfloat16>((int64_t)p.R * p.group, p.dim) : build_of<float>((int64_t)p.R * p.group, p.dim);
   p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;

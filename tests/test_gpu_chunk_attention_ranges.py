@@ -123,3 +123,13 @@ def test_long_caches(ersd, dtype, B, R, Hq, H, D, page, ctx):  # noqa: F811
     check(ersd, *args)
     check(ersd, *args, split=1, window=30000, sinks=64)
     check(ersd, *args, max_context=100)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [80, 256])
+@pytest.mark.parametrize("R,Hq,H", [(9, 8, 2), (37, 2, 2), (12, 8, 2), (7, 7, 1), (16, 8, 2)])
+def test_few_and_many_rows_of_other_heads(ersd, dtype, D, R, Hq, H):  # noqa: F811
+    """Either side of where the kernels of 32-bit arithmetic change: 36 rows of bfloat16, 48 of float32."""
+    check(ersd, *make(2, R, Hq, H, D, 16, [200, 31], dtype))
+    few = R * (Hq // H) <= (48 if dtype == torch.float32 else 36)
+    assert ("rows_kernel" if few else "tile_kernel") in ersd.ersd_last_launch()
