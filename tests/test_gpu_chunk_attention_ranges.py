@@ -133,3 +133,15 @@ def test_few_and_many_rows_of_other_heads(ersd, dtype, D, R, Hq, H):  # noqa: F8
     check(ersd, *make(2, R, Hq, H, D, 16, [200, 31], dtype))
     few = R * (Hq // H) <= (48 if dtype == torch.float32 else 36)
     assert ("rows_kernel" if few else "tile_kernel") in ersd.ersd_last_launch()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("Hq,R", [(71, 1), (71, 5), (300, 1), (300, 9)])
+def test_many_heads_share_one(ersd, dtype, Hq, R):  # noqa: F811
+    """More query heads to a kv head than a tile has rows."""
+    args = make(2, R, Hq, 1, 64, 16, [250, 31], dtype)
+    check(ersd, *args)
+    if R == 9:
+        rows = torch.tensor([4, 9], dtype=torch.int32, device="cuda")
+        poison_behind(*args[1:], rows, R)
+        check(ersd, *args, rows, parent=TREES["star"], window=20, sinks=1)
