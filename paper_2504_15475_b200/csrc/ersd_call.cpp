@@ -172,6 +172,11 @@ std::vector<int32_t> parents(PyObject* o, int nodes) {
       Py_DECREF(seq);
       throw Failed();
     }
+    if (v < INT32_MIN || v > INT32_MAX) {
+      Py_DECREF(seq);
+      PyErr_SetString(PyExc_ValueError, "parent has an entry that is no 32-bit number");
+      throw Failed();
+    }
     p[i] = (int32_t)v;
   }
   Py_DECREF(seq);

@@ -58,3 +58,17 @@ def test_expanded_tensors_are_read_but_not_written(ersd):
             with pytest.raises(ersd.ErsdError) as e:
                 call()
             assert e.value.status == -1
+
+
+def test_parents_beyond_32_bits(ersd):
+    """Numbers that 32 bits do not hold are no nodes, whatever their lower bits say."""
+    k = torch.zeros(4, 16, 2, 64, device="cuda")
+    table, lens = torch.zeros(1, 4, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = torch.ones(1, 3, 4, 64, device="cuda")
+    x = torch.zeros(1, 3, 100, device="cuda")
+    drafts = torch.zeros(1, 3, dtype=torch.int32, device="cuda")
+    for parent in ([-1, 2 ** 32, 0], [2 ** 32 - 1, 0, 0], [-1, 0, -2 ** 32], [-1, 0, 2 ** 40 + 1]):
+        with pytest.raises(ValueError):
+            ersd.ersd_chunk_attention(q, k, k, table, lens, torch.empty_like(q), parent=parent)
+        with pytest.raises(ValueError):
+            ersd.ersd_process_logits(x, torch.empty_like(x), draft_tokens=drafts, parent=parent)
