@@ -407,7 +407,8 @@ typedef struct ersd_chunk_opts {
  * Row n sees the slots below context_lens[b], itself and: every row before it (parent NULL) or its
  * ancestors (a tree); of these, with a window, those whose position is > its own - window or < sinks.
  * A row that sees nothing gets zeros.  Slots that no row of a call sees do not enter, whatever they
- * hold, and pages of such slots alone are not read.
+ * hold, and pages of such slots alone are not read.  (A slot that some row sees takes part in the others with
+ * weight 0, as in a softmax of masked scores: an infinity or NaN among its values reaches them.)
  *   q device [B, R, Hq, head_dim]   out device [B, R, Hq, head_dim]   of cache->dtype, not overlapping
  *   context_lens device [B] int32
  * Scores, softmax and sums are 32-bit.  bfloat16 caches with head_dim 64 or 128, page_size a multiple

@@ -10,22 +10,31 @@
 //            products, since what bounds a tile is the waits of the one that issues.  Either 64 slots at a time
 //            with half of an SM's shared and tensor memory, so that two blocks share an SM and one's start and end
 //            hide behind the other; or, for calls of no more blocks than SMs, 128 slots at a time with longer rings,
-//            four warps that copy and q in tensor memory (from shared memory it takes 96 cycles for every 64 columns,
-//            from there 32).  The product has 128 rows whether they are there or not: up to 32 rows are put there
+//            four warps that copy and q in tensor memory, which leaves shared memory and its rate to them (a step of 16
+//            by itself: 64 cycles for 128 columns from either; for 64 columns 48 from shared memory, 32 from there).  The product has 128 rows whether they are there or not: up to 32 rows are put there
 //            four times, up to 64 twice, and each copy's warps take a part of the slots, which divides the softmax's
 //            time (a warp's powers of two for 64 slots alone take 512 cycles) by as much; the copies' outputs are
 //            joined at the end.
 //   Many<D>  256 packed rows (long chunks), where products and powers of two do: two streams of 128 rows with a
-//            softmax group each, 128 slots at a time (with 64 the first operand, read again for every 64 columns,
-//            takes more of shared memory's rate than there is: 2545 cycles for 64 slots against 3660 for 128); one's
+//            softmax group each, 128 slots at a time (with 64 the first operand is read again for every 64 columns: a
+//            score product by itself takes 384 cycles for 64 slots, 512 for 128, and the kernel 2545 against 3660); one's
 //            products run while the other's softmax does, and half of a tile's weights go ahead of the rest.
-//            Of 3170 cycles for a tile of heads of 128 the products take 97 % (1024 for a stream's scores, at half the
-//            rate for want of shared memory's, 512 for its outputs); of 2970 with heads of 64 powers of two take 2048.
+//            No unit is at its limit: of 3170 cycles for a tile of heads of 128 the tensor cores are busy 2048 (scores and
+//            outputs of a stream 512 each, measured by themselves), powers of two take 2048, shared memory's traffic at
+//            128 bytes a cycle 2048.  What takes the time is a stream's chain, whose scores take the place of its weights:
+//            scores 512, softmax 1850 to 1950, the second half of the outputs 256, and waits for the other stream's
+//            products in the one queue.  (Over the prompt below the tensor cores are busy 57 % of the cycles in which an SM has a block,
+//            which is 85 % of the call: 512 blocks of unlike length, 3.5 to an SM.)  With heads of 64 a tile takes 2970, products 1024 and powers of two 2048 of them.
 //            (q in tensor memory, which has room for it beside 64 slots: 683 us instead of 580 for the prompt below.)
-// Measured on one B200: 32 trees of 17 nodes behind 3100 positions on average (32/8 heads of 128) 80 us, 5.1 TB/s
-// of cache; one token each in 18 sequences behind 64000 positions 702 us, 6.7 TB/s (behind 32000 to 64000: 592
-// us, 6.0); one token behind 1000 positions 9.2 us; 2 x 2048 rows behind up to 8192 positions 525 to 590 us, 0.93 to 1.05
-// PFLOP/s.
+// Measured on one B200 (several of them where a range is given): 32 trees of 17 nodes behind 3100 positions on average
+// (32/8 heads of 128) 79 to 91 us, 4.6 to 5.3 TB/s; one token each in 18 sequences behind 64000 positions 702 us, 6.7 TB/s
+// (behind 32000 to 64000: 568 to 592 us, 6.1 to 6.3); one token behind 1000 positions 9.2 to 9.5 us, behind 64000 54 to 60 us; 2 x
+// 2048 rows behind up to 8192 positions 519 to 607 us, 0.91 to 1.06 PFLOP/s (heads of 64: 481 us).
+//
+// The second product takes both operands in one type, and values are bfloat16: weights are rounded to bfloat16 for it, by
+// 2^-8 of each at most.  Sums are of the unrounded weights (of the rounded ones the result is as far off).  Against 64 bits
+// the result is 1.2 to 1.4 times as far off as its own rounding to bfloat16 leaves it; weights in two parts would
+// take that product twice.  kernel_path = 1 rounds no weight.
 //
 // The output's accumulator stays in tensor memory.  It is scaled only when a row's maximum has risen by more than
 // 2^8 since the last time (weights are then at most 2^8, which bfloat16 and the 32-bit sums hold as well as 1);
@@ -980,7 +989,7 @@ int launch_attention_tensor(AttentionParams& p, int max_context, cudaStream_t st
   p.row_tiles = (int)(((int64_t)p.R * p.group + (many ? 255 : 127)) / (many ? 256 : 128));
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
   // Blocks with a long ring while no more than one goes to an SM (18 sequences of 32000 to 64000 positions, 144
-  // blocks: 620 us; 1150 with the shorter rings and one block to an SM),
+  // blocks, when the two were compared: 620 us, and 1150 with the shorter rings and one block to an SM),
   // else two to an SM.
   const bool alone = many || units * (p.split ? p.split : 1) <= sms;
   const int at = (p.dim == 64 ? 0 : 3) + (many ? 2 : alone ? 1 : 0);

@@ -9,8 +9,9 @@
 // chunk away.  A chunk of which the mask allows nothing is not read.
 //
 // Measured on one B200, bfloat16: 64 chains of nine rows x 128256 tokens behind up to 4096 tokens, all penalties and 64 biases,
-// 67 us (4.4 TB/s; without any change 48 us: instructions for the slices of the frequent tokens are the rest); 32
-// trees of 17 rows x 151936 under masks 81 us (68 without penalties); one float32 row of 32000 in 4.1 us.
+// 67 us (4.4 TB/s; without any change 48 us: the rest is latency, a lane's listed tokens one after the other in every row,
+// with an instruction issued in half of the cycles); 32 trees of 17 rows x 151936 under masks 81 us (68 without
+// penalties); one float32 row of 32000 in 4.1 us.
 // Counts of 4096 tokens by each block that shares a sequence's rows are what a small batch costs: one such chain 10.8 us.
 #include <cuda_bf16.h>
 #include <math.h>
