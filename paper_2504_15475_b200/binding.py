@@ -344,7 +344,7 @@ def ersd_cache_commit(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table:
                       stream=None) -> None:
     """After a tree verification: the accepted nodes' keys and values (path int32 [B, D+1]: its opts.out_path) move
     to the slots behind the context, in all layers of caches [layers, pages, page_size, heads, D] (or one, without
-    the first dimension); out_context_lens int32 [B] = context_lens + accept_len + 1."""
+    the first dimension); out_context_lens int32 [B], memory of its own, = context_lens + accept_len + 1."""
     status = (_native or native()).cache_commit(k_cache, v_cache, block_table, context_lens, path, accept_len, out_context_lens,
                                                 stream)
     if status:
