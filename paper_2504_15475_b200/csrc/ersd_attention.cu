@@ -547,16 +547,22 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) rows_kernel(const Attention
 }
 
 // Up to how many packed rows of a kv head rows_kernel takes, which goes through the cache once for every four, while
-// tile_kernel's tiles are of 64 whether the rows are there or not (rows_kernel / tile_kernel, us):
+// tile_kernel's tiles are of 64 whether the rows are there or not, and no more than eight blocks share one.  `heads`: of
+// all sequences (rows_kernel / tile_kernel, us):
 //                                            36 rows        48 rows      bfloat16: 36 rows    48 rows
-//   8 x 777 positions, 16 heads of 64         72 / 91       103 / 91          93 / 93         136 / 94
+//   1 x 20000 positions, 2 heads of 96       135 / 509      133 / 510        162 / 568        162 / 569
+//   1 x 2000, 8 heads of 96                   54 / 57        57 / 58          68 / 63          69 / 64
+//   1 x 8000, 8 heads of 256                 330 / 466      355 / 472        411 / 407        493 / 409
 //   2 x 300, 8 heads of 64                    11 / 23        13 / 23          13 / 24          15 / 24
-//   32 x 3000, 8 heads of 64                 549 / 651      788 / 652        949 / 704       1359 / 701
-//   8 x 1500, 8 heads of 80                  159 / 166      310 / 169        193 / 183        368 / 184
+//   2 x 2000, 8 heads of 256                 153 / 200      174 / 203        201 / 215        218 / 219
+//   4 x 2000, 8 heads of 96                  108 / 169      204 / 171        131 / 188        253 / 190
 //   4 x 1500, 8 heads of 128                  69 / 131      125 / 133         87 / 142        166 / 144
-//   16 x 3000, 8 heads of 128                544 / 756      776 / 759        938 / 899       1375 / 900
 //   4 x 1500, 8 heads of 256                 141 / 276      277 / 286        167 / 250        325 / 254
-constexpr int few_rows(bool bf16) { return bf16 ? 36 : 48; }
+//   8 x 1500, 8 heads of 80                  159 / 166      310 / 169        193 / 183        368 / 184
+//   8 x 777, 16 heads of 64                   72 / 91       103 / 91          93 / 93         136 / 94
+//   16 x 3000, 8 heads of 128                544 / 756      776 / 759        938 / 899       1375 / 900
+//   32 x 3000, 8 heads of 64                 549 / 651      788 / 652        949 / 704       1359 / 701
+constexpr int few_rows(bool bf16, int64_t heads) { return bf16 && heads > 16 ? 36 : 48; }
 
 struct Build {
   const void* kernel;
@@ -571,16 +577,16 @@ Build rows_build(int dim) {
   return {(const void*)rows_kernel<T, 32, MR>, sizeof(RowShared<32, MR>), MR, kThreadsFew, kSlots};
 }
 template <typename T>
-Build build_of(int64_t rows, int dim) {
-  if (rows <= few_rows(sizeof(T) == 2)) return rows_build<T, kRows>(dim);
+Build build_of(bool few, int dim) {
+  if (few) return rows_build<T, kRows>(dim);
   if (dim <= 64) return {(const void*)tile_kernel<T, 64, 64>, sizeof(Shared<64, 64>), 64, kThreads, kNK};
   if (dim <= 128) return {(const void*)tile_kernel<T, 64, 128>, sizeof(Shared<64, 128>), 64, kThreads, kNK};
   return {(const void*)tile_kernel<T, 64, 256>, sizeof(Shared<64, 256>), 64, kThreads, kNK};
 }
 
 int launch_attention_f32(AttentionParams& p, bool bf16, int max_context, cudaStream_t st) {
-  const bool few = (int64_t)p.R * p.group <= few_rows(bf16);
-  const Build k = bf16 ? build_of<__nv_bfloat16>((int64_t)p.R * p.group, p.dim) : build_of<float>((int64_t)p.R * p.group, p.dim);
+  const bool few = (int64_t)p.R * p.group <= few_rows(bf16, (int64_t)p.heads * p.B);
+  const Build k = bf16 ? build_of<__nv_bfloat16>(few, p.dim) : build_of<float>(few, p.dim);
   p.row_tiles = (int)(((int64_t)p.R * p.group + k.rows - 1) / k.rows);
   const int64_t units = (int64_t)p.row_tiles * p.heads * p.B;
   if (!p.split) {

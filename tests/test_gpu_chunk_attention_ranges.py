@@ -129,10 +129,11 @@ def test_long_caches(ersd, dtype, B, R, Hq, H, D, page, ctx):  # noqa: F811
 @pytest.mark.parametrize("D", [80, 256])
 @pytest.mark.parametrize("R,Hq,H", [(9, 8, 2), (37, 2, 2), (12, 8, 2), (7, 7, 1), (16, 8, 2)])
 def test_few_and_many_rows_of_other_heads(ersd, dtype, D, R, Hq, H):  # noqa: F811
-    """Either side of where the kernels of 32-bit arithmetic change: 36 rows of bfloat16, 48 of float32."""
-    check(ersd, *make(2, R, Hq, H, D, 16, [200, 31], dtype))
-    few = R * (Hq // H) <= (48 if dtype == torch.float32 else 36)
-    assert ("rows_kernel" if few else "tile_kernel") in ersd.ersd_last_launch()
+    """Either side of where the kernels of 32-bit arithmetic change: 48 rows, with bfloat16 36 from 17 heads on."""
+    for B in (2, 18):
+        check(ersd, *make(B, R, Hq, H, D, 16, [200, 31] * (B // 2), dtype))
+        most = 36 if dtype == torch.bfloat16 and B * H > 16 else 48
+        assert ("rows_kernel" if R * (Hq // H) <= most else "tile_kernel") in ersd.ersd_last_launch()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
